@@ -425,6 +425,110 @@ int es_spmm_launch_info(int64_t N, int64_t nnz, int32_t F, int32_t ldx, int32_t 
                         int32_t mode, int32_t aligned16, int32_t backward,
                         const es_launch_opts_t* opts, es_launch_info_t* info);
 
+/*
+ * 8-bit rows.  A table of N rows of F numbers held as int8 codes with one fp32 scale
+ * per row: a layer's input kept for the backward pass, or a table of features or of
+ * past embeddings that a serving program keeps, in a quarter of the bytes.  A row x is
+ * held as
+ *     scale   = max|x| / 127, rounded to fp32 (and at most the largest number whose
+ *               127-fold is finite)
+ *     code[c] = x[c] / scale rounded to the nearest integer, ties to even (of the
+ *               exact quotient: the codes do not depend on the machine)
+ * and stands for the values scale * code[c].  A row whose largest magnitude is below
+ * 127 * 2^-126 is held as zeros; a row that holds an infinity or a NaN has the scale
+ * NaN and stands for NaN in every column.  No other value is ever clipped.
+ *   codes  [N x ldq] int8 (device), 16-byte aligned, ldq a multiple of 16 and >= F;
+ *          es_q8_row_bytes(F) is the smallest, F rounded up to 16.  Columns F to
+ *          es_q8_row_bytes(F) - 1 are written as 0; readers ignore them.  N < 2^31.
+ *   scale  [N] fp32 (device)
+ * Dense matrices beside the table may have any row stride >= their width and any
+ * alignment of their elements' size.
+ */
+typedef enum { ES_FP32 = 0, ES_FP16 = 1, ES_BF16 = 2 } es_type_t;
+
+int32_t es_q8_row_bytes(int32_t F);   /* 0 for F < 1 or F > 2^31 - 16 */
+
+/*
+ * es_q8_write -- writes n rows into the table.
+ *   X      n rows of F elements of `type` (an es_type_t), row stride ldx >= F elements
+ *   rows   [n] int32 (device): row i of X becomes row rows[i] of the table; NULL: row i
+ *          (n <= N).  An id outside [0, N) is skipped (a padded batch).  Where an id
+ *          occurs more than once its last row is the one that is written.
+ * Rows of the table that are not named keep their contents.
+ */
+int es_q8_write(const void* X, int32_t type, int64_t n, int32_t F, int32_t ldx,
+                const int32_t* rows, int64_t N, int8_t* codes, int32_t ldq, float* scale,
+                void* stream);
+
+/*
+ * es_q8_read -- reads n rows of the table back.
+ *   rows   [n] int32 (device): row i of Y becomes row rows[i] of the table; NULL: row i
+ *          (n <= N).  An id outside [0, N) gives a row of zeros.
+ *   Y      n rows of F elements of `type`, row stride ldy >= F, written; a value is
+ *          rounded once, from fp32 to the nearest of `type`, ties to even.
+ */
+int es_q8_read(const int8_t* codes, int32_t ldq, const float* scale, int64_t N, int32_t F,
+               const int32_t* rows, int64_t n, void* Y, int32_t type, int32_t ldy,
+               void* stream);
+
+/*
+ * es_spmm_q8 -- es_spmm_norm on a table of 8-bit rows, for all rows or for some: the
+ * gathered rows are what bounds the product, and they are a quarter as large.
+ *     Y[i, c] = f_r * sum over the kept slots of row r = rows[i] of
+ *               vals[p] * scale[colidx[p]] * code[colidx[p], c]
+ * Sampling, values, norms and the graph's arrays as in es_spmm_norm; a FastRand rotation
+ * goes by the row r of the graph, so an asked row is the same as in a product of all.
+ *   rows    [n_rows] int32 (device): the rows asked for, in any order, also more than
+ *           once (serving: the batch's nodes); an id outside [0, N) gives a row of
+ *           zeros.  NULL: all rows, n_rows == N.
+ *   Y       n_rows rows of F fp32, row stride ldy >= F, overwritten
+ *   nnz     rowptr[N], a launch-shape hint as in es_spmm
+ * Accumulation is fp32 in a fixed order: the same call gives the same bits.  A row of
+ * the table that no kept entry names has no influence, whatever it holds.
+ */
+int es_spmm_q8(const int32_t* rowptr, const int32_t* colidx, const float* vals,
+               const int8_t* codes, int32_t ldq, const float* scale, float* Y,
+               int64_t N, int64_t nnz, int32_t F, int32_t ldy, int32_t W, int32_t mode,
+               uint64_t seed, int32_t norm, const int32_t* rows, int64_t n_rows,
+               void* stream);
+
+/*
+ * es_spmm_q8_backward_vals -- the gradient of the product with respect to `vals`, for
+ * learned edge values: the part of the backward pass that reads the product's input,
+ * here from its 8-bit checkpoint.  (The gradient with respect to the input is
+ * es_spmm_backward's and does not read it.)
+ *     dvals[p] = f_r * scale[c] * sum over columns of dY[r, :] * code[c, :]
+ * for the entries p = (r, c) that W, mode and seed keep, 0 for the others.
+ *   dY      N rows of F fp32, row stride ldy >= F (input)
+ *   dvals   [nnz] fp32, entries rowptr[0] to rowptr[N] - 1 written
+ *   nnz     rowptr[N], a launch-shape hint; 0: no entries, nothing is written
+ * Sums are fp32 in a fixed order.
+ */
+int es_spmm_q8_backward_vals(const int32_t* rowptr, const int32_t* colidx,
+                             const float* dY, int32_t ldy, const int8_t* codes, int32_t ldq,
+                             const float* scale, float* dvals, int64_t N, int64_t nnz,
+                             int32_t F, int32_t W, int32_t mode, uint64_t seed, int32_t norm,
+                             void* stream);
+
+/*
+ * es_q8_weight_grad -- dW = X^T * G with X held as 8-bit rows: the weight gradient of a
+ * dense layer Z = X * W (Equation 1's H * W) from the checkpoint of its input.
+ *   G       N rows of H fp32, row stride ldg >= H: the gradient with respect to Z
+ *   dW      F rows of H fp32, row stride ldw >= H, overwritten (zeros for N == 0)
+ *   workspace  es_q8_weight_grad_workspace_bytes(N, F, H) bytes (0: none is of use),
+ *           16-byte aligned; contents on entry are irrelevant, on return unspecified;
+ *           calls that share it must be ordered (same stream).  With a smaller one,
+ *           or none, each element is summed by one workgroup: right, but slow for
+ *           many rows.
+ * Sums are fp32 in an order that the sizes and the workspace fix.
+ */
+size_t es_q8_weight_grad_workspace_bytes(int64_t N, int32_t F, int32_t H);
+
+int es_q8_weight_grad(const int8_t* codes, int32_t ldq, const float* scale,
+                      const float* G, int32_t ldg, float* dW, int32_t ldw,
+                      int64_t N, int32_t F, int32_t H,
+                      void* workspace, size_t workspace_bytes, void* stream);
+
 /* Human-readable name of a status code (static storage, never NULL). */
 const char* es_spmm_status_string(int status);
 

@@ -11,6 +11,7 @@ from typing import Optional
 ES_FULL, ES_BUCKET, ES_FASTRAND = 0, 1, 2
 MODES = {"full": ES_FULL, "bucket": ES_BUCKET, "fastrand": ES_FASTRAND}
 ES_NORM_NONE, ES_NORM_MEAN, ES_NORM_RSQRT, ES_NORM_RESCALE, ES_NORM_INV_DEGREE = 0, 1, 2, 3, 4
+ES_FP32, ES_FP16, ES_BF16 = 0, 1, 2
 NORMS = {"none": ES_NORM_NONE, "mean": ES_NORM_MEAN, "rsqrt": ES_NORM_RSQRT, "rescale": ES_NORM_RESCALE,
          "inv_degree": ES_NORM_INV_DEGREE}
 
@@ -114,6 +115,22 @@ def load_library():
     lib.es_spmm_launch_info.argtypes = [ctypes.c_int64, ctypes.c_int64, ctypes.c_int32, ctypes.c_int32,
                                         ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32,
                                         ctypes.c_int32, optp, ctypes.POINTER(es_launch_info_t)]
+    i32, i64, size_t = ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
+    lib.es_q8_row_bytes.restype = i32
+    lib.es_q8_row_bytes.argtypes = [i32]
+    lib.es_q8_write.restype = ctypes.c_int
+    lib.es_q8_write.argtypes = [vp, i32, i64, i32, i32, vp, i64, vp, i32, vp, vp]
+    lib.es_q8_read.restype = ctypes.c_int
+    lib.es_q8_read.argtypes = [vp, i32, vp, i64, i32, vp, i64, vp, i32, i32, vp]
+    lib.es_spmm_q8.restype = ctypes.c_int
+    lib.es_spmm_q8.argtypes = [vp, vp, vp, vp, i32, vp, vp, i64, i64, i32, i32, i32, i32, ctypes.c_uint64, i32, vp, i64, vp]
+    lib.es_spmm_q8_backward_vals.restype = ctypes.c_int
+    lib.es_spmm_q8_backward_vals.argtypes = [vp, vp, vp, i32, vp, i32, vp, vp, i64, i64, i32, i32, i32, ctypes.c_uint64,
+                                             i32, vp]
+    lib.es_q8_weight_grad_workspace_bytes.restype = size_t
+    lib.es_q8_weight_grad_workspace_bytes.argtypes = [i64, i32, i32]
+    lib.es_q8_weight_grad.restype = ctypes.c_int
+    lib.es_q8_weight_grad.argtypes = [vp, i32, vp, vp, i32, vp, i32, i64, i32, i32, vp, size_t, vp]
     lib.es_spmm_status_string.restype = ctypes.c_char_p
     lib.es_spmm_status_string.argtypes = [ctypes.c_int]
     lib.es_spmm_max_W.restype = ctypes.c_int32
@@ -552,3 +569,206 @@ def es_spmm_validate_csr(rowptr, colidx, report=None, stream=None):
     if rc != 0:
         raise EsSpmmError(rc, "es_spmm_validate_csr")
     return report
+
+
+# ---- 8-bit rows -------------------------------------------------------------------------------
+def _types():
+    import torch
+    return {torch.float32: ES_FP32, torch.float16: ES_FP16, torch.bfloat16: ES_BF16}
+
+
+def _here(stream, **tensors):
+    """The tensors are on the current device and can be read; returns the stream's address."""
+    import torch
+    m = _marshal or load_marshal()
+    for name, t in tensors.items():
+        if t is None:
+            continue
+        if not isinstance(t, torch.Tensor) or not t.is_cuda:
+            raise ValueError(f"{name} must be a device tensor")
+        if t.get_device() != torch.cuda.current_device():
+            raise ValueError(f"{name} is on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+        if not m.readable(t):
+            raise ValueError(f"{name} has no device memory of its own (a fake, sparse or wrapped tensor)")
+    return _stream_ptr(stream)
+
+
+def _matrix(t, name, columns=None):
+    """(rows, columns, row stride) of a dense matrix with unit column stride."""
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name} must be 2-D with contiguous columns")
+    if columns is not None and t.shape[1] != columns:
+        raise ValueError(f"{name} must have {columns} columns, has {t.shape[1]}")
+    ld = t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    if t.shape[0] > 0 and not t.shape[1] <= ld < 2 ** 31:
+        raise ValueError(f"{name} has rows that overlap, or a row stride of 2^31 and more")
+    return t.shape[0], t.shape[1], max(int(ld), t.shape[1])
+
+
+def _table(codes, scale, F):
+    """(N, ldq) of a table of 8-bit rows of F numbers."""
+    import torch
+    if codes.dtype != torch.int8 or scale.dtype != torch.float32:
+        raise ValueError("codes must be int8 and scale float32")
+    N, width, ldq = _matrix(codes, "codes")
+    row = int(load_library().es_q8_row_bytes(int(F)))
+    if width < row or ldq % 16 or codes.data_ptr() % 16:
+        raise ValueError(f"codes must hold es_q8_row_bytes({F}) = {row} columns, 16-byte aligned, with a row stride that "
+                         f"is a multiple of 16")
+    if scale.dim() != 1 or scale.shape[0] != N or (N > 1 and scale.stride(0) != 1):
+        raise ValueError("scale must be contiguous, one number per row of codes")
+    return N, ldq
+
+
+def _ids(rows, n, name="rows"):
+    import torch
+    if rows is None:
+        return None
+    if rows.dtype != torch.int32 or rows.dim() != 1 or rows.shape[0] != n or not rows.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous int32 vector of {n} ids")
+    return rows.data_ptr() or None
+
+
+def _type_code(t, name):
+    code = _types().get(t.dtype)
+    if code is None:
+        raise ValueError(f"{name} must be float32, float16 or bfloat16, is {t.dtype}")
+    return code
+
+
+def _norm(norm) -> int:
+    return NORMS[norm] if isinstance(norm, str) else int(norm)
+
+
+def _checked(rc, where):
+    if rc != 0:
+        raise EsSpmmError(rc, where)
+
+
+def es_q8_row_bytes(F: int) -> int:
+    """Bytes of a row of F codes (F rounded up to 16): a table is
+    torch.empty((N, es_q8_row_bytes(F)), dtype=torch.int8) and a float32 scale per row."""
+    return int(load_library().es_q8_row_bytes(int(F)))
+
+
+def es_q8_write(X, codes, scale, rows=None, stream=None):
+    """Writes the rows of X [n, F] (float32, float16 or bfloat16) into the table (codes [N, es_q8_row_bytes(F)]
+    int8, scale [N] float32): row i becomes row rows[i] (int32; ids outside [0, N) are skipped, of
+    equal ids the last row is written), or without `rows` row i.  Returns (codes, scale)."""
+    st = _here(stream, X=X, codes=codes, scale=scale, rows=rows)
+    n, F, ldx = _matrix(X, "X")
+    if F < 1:
+        raise ValueError("X must have at least one column")
+    N, ldq = _table(codes, scale, F)
+    if rows is None and n > N:
+        raise ValueError(f"X has {n} rows, the table {N}")
+    _checked(load_library().es_q8_write(X.data_ptr() or None, _type_code(X, "X"), n, F, ldx, _ids(rows, n), N,
+                                        codes.data_ptr() or None, ldq, scale.data_ptr() or None, st), "es_q8_write")
+    return codes, scale
+
+
+def es_q8_read(codes, scale, Y, rows=None, stream=None):
+    """Reads rows of the table into Y [n, F] (float32, float16 or bfloat16): row rows[i] (int32; ids outside
+    [0, N) give zeros), or without `rows` row i.  Returns Y."""
+    st = _here(stream, codes=codes, scale=scale, Y=Y, rows=rows)
+    n, F, ldy = _matrix(Y, "Y")
+    if F < 1:
+        raise ValueError("Y must have at least one column")
+    N, ldq = _table(codes, scale, F)
+    if rows is None and n > N:
+        raise ValueError(f"Y has {n} rows, the table {N}")
+    _checked(load_library().es_q8_read(codes.data_ptr() or None, ldq, scale.data_ptr() or None, N, F, _ids(rows, n), n,
+                                       Y.data_ptr() or None, _type_code(Y, "Y"), ldy, st), "es_q8_read")
+    return Y
+
+
+def _q8_graph(rowptr, colidx, codes, scale, F):
+    import torch
+    N, ldq = _table(codes, scale, F)
+    for t, name in ((rowptr, "rowptr"), (colidx, "colidx")):
+        if t.dtype != torch.int32 or t.dim() != 1 or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous int32 vector")
+    if rowptr.numel() != N + 1:
+        raise ValueError("the table needs one row per CSR row")
+    return N, ldq
+
+
+def es_spmm_q8(rowptr, colidx, vals, codes, scale, Y, W: int, mode, seed: int = 0, norm="none", rows=None, stream=None):
+    """Y[i] = f * sum of vals[p] * (row colidx[p] of the table) over the kept entries p of row rows[i] (int32 ids
+    in any order; outside [0, N): zeros), or of every row; Y float32 [n, F].  Returns Y."""
+    import torch
+    st = _here(stream, rowptr=rowptr, colidx=colidx, vals=vals, codes=codes, scale=scale, Y=Y, rows=rows)
+    n, F, ldy = _matrix(Y, "Y")
+    if F < 1 or Y.dtype != torch.float32:
+        raise ValueError("Y must be float32 with at least one column")
+    N, ldq = _q8_graph(rowptr, colidx, codes, scale, F)
+    if rows is None and n != N:
+        raise ValueError("Y needs one row per CSR row")
+    if vals is not None and (vals.dtype != torch.float32 or vals.numel() != colidx.numel() or not vals.is_contiguous()):
+        raise ValueError("vals must be contiguous float32, one per entry of colidx")
+    _checked(load_library().es_spmm_q8(
+        rowptr.data_ptr() or None, colidx.data_ptr() or None, None if vals is None else vals.data_ptr() or None,
+        codes.data_ptr() or None, ldq, scale.data_ptr() or None, Y.data_ptr() or None, N, colidx.numel(), F, ldy, int(W),
+        _mode(mode), int(seed) & 0xFFFFFFFFFFFFFFFF, _norm(norm), _ids(rows, n), n, st), "es_spmm_q8")
+    return Y
+
+
+def es_spmm_q8_backward_vals(rowptr, colidx, dY, codes, scale, dvals, W: int, mode, seed: int = 0, norm="none", stream=None):
+    """dvals[p] = f * (dY[r] . row c of the table) for the kept entries p = (r, c), 0 for the others: the gradient of
+    es_spmm_q8's and es_spmm_norm's Y with respect to `vals`; dY float32 [N, F], dvals float32 [nnz].  Returns dvals."""
+    import torch
+    st = _here(stream, rowptr=rowptr, colidx=colidx, dY=dY, codes=codes, scale=scale, dvals=dvals)
+    n, F, ldy = _matrix(dY, "dY")
+    if F < 1 or dY.dtype != torch.float32:
+        raise ValueError("dY must be float32 with at least one column")
+    N, ldq = _q8_graph(rowptr, colidx, codes, scale, F)
+    if n != N:
+        raise ValueError("dY needs one row per CSR row")
+    if dvals.dtype != torch.float32 or dvals.numel() != colidx.numel() or not dvals.is_contiguous():
+        raise ValueError("dvals must be contiguous float32, one per entry of colidx")
+    _checked(load_library().es_spmm_q8_backward_vals(
+        rowptr.data_ptr() or None, colidx.data_ptr() or None, dY.data_ptr() or None, ldy, codes.data_ptr() or None, ldq,
+        scale.data_ptr() or None, dvals.data_ptr() or None, N, colidx.numel(), F, int(W), _mode(mode),
+        int(seed) & 0xFFFFFFFFFFFFFFFF, _norm(norm), st), "es_spmm_q8_backward_vals")
+    return dvals
+
+
+def es_q8_weight_grad_workspace_bytes(N: int, F: int, H: int) -> int:
+    return int(load_library().es_q8_weight_grad_workspace_bytes(int(N), int(F), int(H)))
+
+
+def es_q8_weight_grad(codes, scale, G, dW, workspace=None, stream=None):
+    """dW [F, H] = (the table's N rows of F values)^T @ G [N, H], float32.  `workspace`: a contiguous device tensor of
+    es_q8_weight_grad_workspace_bytes(N, F, H) bytes; by default one from torch's allocator.  Returns dW."""
+    import torch
+    st = _here(stream, codes=codes, scale=scale, G=G, dW=dW, workspace=workspace)
+    n, H, ldg = _matrix(G, "G")
+    F, _, ldw = _matrix(dW, "dW", H)
+    if F < 1 or H < 1 or G.dtype != torch.float32 or dW.dtype != torch.float32:
+        raise ValueError("G and dW must be float32 with at least one row of dW and one column")
+    N, ldq = _table(codes, scale, F)
+    if n != N:
+        raise ValueError("G needs one row per row of codes")
+    lib = load_library()
+    if workspace is None:
+        need = int(lib.es_q8_weight_grad_workspace_bytes(N, F, H))
+        if need:
+            with torch.cuda.stream(_torch_stream(stream)):
+                workspace = torch.empty(need, dtype=torch.uint8, device=G.device)
+    elif not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous device tensor")
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _checked(lib.es_q8_weight_grad(codes.data_ptr() or None, ldq, scale.data_ptr() or None, G.data_ptr() or None, ldg,
+                                   dW.data_ptr() or None, ldw, N, F, H, workspace.data_ptr() if ws_bytes else None, ws_bytes,
+                                   st), "es_q8_weight_grad")
+    return dW
+
+
+def _torch_stream(stream):
+    """A stream of torch for None, an address or a stream, so that memory comes from that stream's pool."""
+    import torch
+    if stream is None:
+        return torch.cuda.current_stream()
+    if isinstance(stream, int):
+        return torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
+    return stream

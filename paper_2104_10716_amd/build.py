@@ -5,10 +5,11 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import tempfile
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
-SRC = os.path.join(PKG, "csrc", "es_spmm.hip")
+SOURCES = [os.path.join(PKG, "csrc", name) for name in ("es_spmm.hip", "es_q8.hip")]
 LIB = os.path.join(PKG, "libes_spmm.so")
 MARSHAL_SRC = os.path.join(PKG, "csrc", "es_marshal.cpp")
 MARSHAL = os.path.join(PKG, "_es_marshal.so")
@@ -27,17 +28,30 @@ def build(verbose: bool = False, out: str = LIB, extra_flags=()) -> str:
     """Compile the library to `out` (default: in-tree).  `extra_flags` are added
     to the hipcc line (host-side instrumentation for the sanitizer test)."""
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    cmd = [hipcc] + HIPCC_FLAGS + list(extra_flags) + [SRC, "-o", out]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    res = subprocess.run(cmd, capture_output=True, text=True)
-    noise = "is not a recognized feature for this target"
-    err = "\n".join(l for l in res.stderr.splitlines() if noise not in l)
-    if res.returncode != 0:
-        raise RuntimeError("hipcc failed:\n" + res.stderr)
-    if verbose and err.strip():
-        print(err, file=sys.stderr)
+    with tempfile.TemporaryDirectory() as tmp:
+        objects = [os.path.join(tmp, os.path.basename(src) + ".o") for src in SOURCES]
+        compile_flags = [f for f in HIPCC_FLAGS if f != "-shared"] + list(extra_flags)
+        link_flags = ["--offload-arch=gfx950", "-shared"] + [f for f in extra_flags if f not in ("-g",)]
+        commands = [[hipcc] + compile_flags + ["-c", src, "-o", obj] for src, obj in zip(SOURCES, objects)]
+        _run_all(commands, verbose)                      # side by side
+        _run_all([[hipcc] + link_flags + objects + ["-o", out]], verbose)
     return out
+
+
+def _run_all(commands, verbose):
+    running = []
+    for cmd in commands:
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        running.append(subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True))
+    outputs = [p.communicate()[0] for p in running]
+    for p, output in zip(running, outputs):
+        if p.returncode != 0:
+            raise RuntimeError("hipcc failed:\n" + output)
+        noise = "is not a recognized feature for this target"
+        err = "\n".join(l for l in output.splitlines() if noise not in l)
+        if verbose and err.strip():
+            print(err, file=sys.stderr)
 
 
 def build_marshal(verbose: bool = False, out: str = MARSHAL) -> str:

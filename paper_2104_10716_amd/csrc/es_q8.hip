@@ -1,0 +1,251 @@
+// es_q8.hip -- the entry points on 8-bit rows (include/es_spmm.h): argument checks and launches.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "es_spmm.h"
+
+#include "es_common.h"
+#include "es_q8_rows.h"
+#include "es_q8_spmm.h"
+#include "es_q8_grad.h"
+
+namespace {
+
+constexpr int32_t kMaxF = INT32_MAX - 15;
+
+int element_bytes(int32_t type) { return type == ES_FP32 ? 4 : type == ES_FP16 || type == ES_BF16 ? 2 : 0; }
+
+bool misaligned(const void* p, uintptr_t to) { return reinterpret_cast<uintptr_t>(p) % to != 0; }
+
+// A table of 8-bit rows as every entry point takes it.
+int check_table(int64_t N, int32_t F, int32_t ldq)
+{
+    if (N < 0 || N > INT32_MAX || F < 1 || F > kMaxF || ldq % 16 || ldq < F) return ES_ERR_INVALID_ARG;
+    return ES_OK;
+}
+
+bool bad_table(const int8_t* codes, const float* scale)
+{
+    return !codes || !scale || misaligned(codes, 16) || misaligned(scale, 4);
+}
+
+int next_pow2(int64_t v)
+{
+    int p = 1;
+    while (p < v) p <<= 1;
+    return p;
+}
+
+int launched() { return hipGetLastError() == hipSuccess ? ES_OK : ES_ERR_LAUNCH; }
+
+bool grid_of(int64_t items, int64_t per_block, uint32_t* out)
+{
+    const int64_t blocks = (items + per_block - 1) / per_block;
+    if (blocks < 1 || blocks > INT32_MAX) return false;
+    *out = (uint32_t)blocks;
+    return true;
+}
+
+template <class T, int MAP>
+int launch_write(const Q8Write& a, hipStream_t st)
+{
+    const int64_t quads = ((int64_t)a.F + 15) / 16 * 4;
+    uint32_t grid;
+#define ES_WRITE(TEAM_, K_, UR_)                                                                                            \
+    if (quads <= (TEAM_) * (K_)) {                                                                                          \
+        if (!grid_of(a.n, (int64_t)(kBlockThreads / (TEAM_)) * (UR_), &grid)) return ES_ERR_UNSUPPORTED;                    \
+        hipLaunchKernelGGL((es_q8_write_kernel<T, TEAM_, K_, UR_, MAP>), dim3(grid), dim3(kBlockThreads), 0, st, a);        \
+        return launched();                                                                                                  \
+    }
+    ES_WRITE(4, 1, 4) ES_WRITE(8, 1, 4) ES_WRITE(16, 1, 4) ES_WRITE(32, 1, 4) ES_WRITE(64, 1, 4)
+    ES_WRITE(64, 2, 2) ES_WRITE(64, 4, 1) ES_WRITE(64, 8, 1)
+#undef ES_WRITE
+    if (!grid_of(a.n, 1, &grid)) return ES_ERR_UNSUPPORTED;
+    hipLaunchKernelGGL((es_q8_write_wide_kernel<T, MAP>), dim3(grid), dim3(kBlockThreads), 0, st, a);
+    return launched();
+}
+
+template <class T>
+int launch_read(const Q8Read& a, hipStream_t st)
+{
+    const int64_t quads = ((int64_t)a.F + 3) / 4;
+    uint32_t grid;
+#define ES_READ(TEAM_)                                                                                                      \
+    if (quads <= (TEAM_) || (TEAM_) == kWaveSize) {                                                                         \
+        if (!grid_of(a.n, (int64_t)(kBlockThreads / (TEAM_)) * 4, &grid)) return ES_ERR_UNSUPPORTED;                        \
+        hipLaunchKernelGGL((es_q8_read_kernel<T, TEAM_, 4>), dim3(grid), dim3(kBlockThreads), 0, st, a);                    \
+        return launched();                                                                                                  \
+    }
+    ES_READ(2) ES_READ(4) ES_READ(8) ES_READ(16) ES_READ(32) ES_READ(64)
+#undef ES_READ
+    return ES_ERR_UNSUPPORTED;
+}
+
+template <class T>
+int run_write(Q8Write a, hipStream_t st)
+{
+    if (!a.rows) return launch_write<T, Q8_ALL>(a, st);
+    if (a.n <= kQ8Scan) return launch_write<T, Q8_SCANNED>(a, st);
+    const size_t row_bytes = (size_t)a.ldx * sizeof(T);
+    const int64_t total = a.n;
+    for (int64_t done = 0; done < total; done += kQ8Claims) {  // in order: a later piece's rows replace an earlier one's
+        Q8Write b = a;
+        b.n = total - done < kQ8Claims ? total - done : kQ8Claims;
+        b.rows = a.rows + done;
+        b.X = static_cast<const char*>(a.X) + (size_t)done * row_bytes;
+        uint32_t grid;
+        if (!grid_of(b.n, kBlockThreads, &grid)) return ES_ERR_UNSUPPORTED;
+        hipLaunchKernelGGL(es_q8_claim_kernel<false>, dim3(grid), dim3(kBlockThreads), 0, st, b);
+        if (launched() != ES_OK) return ES_ERR_LAUNCH;
+        hipLaunchKernelGGL(es_q8_claim_kernel<true>, dim3(grid), dim3(kBlockThreads), 0, st, b);
+        if (launched() != ES_OK) return ES_ERR_LAUNCH;
+        const int rc = launch_write<T, Q8_CLAIMED>(b, st);
+        if (rc != ES_OK) return rc;
+    }
+    return ES_OK;
+}
+
+// What both products on a graph check.
+int check_product(int64_t N, int64_t nnz, int32_t F, int32_t ldq, int32_t ld, int32_t W, int32_t mode, int32_t norm)
+{
+    if (check_table(N, F, ldq) != ES_OK || nnz < 0 || nnz > INT32_MAX || ld < F) return ES_ERR_INVALID_ARG;
+    if (norm < ES_NORM_NONE || norm > ES_NORM_INV_DEGREE) return ES_ERR_INVALID_ARG;
+    if (mode != ES_FULL && mode != ES_BUCKET && mode != ES_FASTRAND) return ES_ERR_INVALID_ARG;
+    if (mode != ES_FULL && W < 1) return ES_ERR_INVALID_ARG;
+    return ES_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int32_t es_q8_row_bytes(int32_t F) { return F < 1 || F > kMaxF ? 0 : (F + 15) / 16 * 16; }
+
+int es_q8_write(const void* X, int32_t type, int64_t n, int32_t F, int32_t ldx, const int32_t* rows, int64_t N,
+                int8_t* codes, int32_t ldq, float* scale, void* stream)
+{
+    const int size = element_bytes(type);
+    if (check_table(N, F, ldq) != ES_OK || !size || n < 0 || n > INT32_MAX || ldx < F || (!rows && n > N)) return ES_ERR_INVALID_ARG;
+    if (n == 0 || N == 0) return ES_OK;
+    if (!X || misaligned(X, size) || bad_table(codes, scale) || misaligned(rows, 4)) return ES_ERR_INVALID_ARG;
+    const Q8Write a = {X, rows, codes, scale, n, N, F, ldx, ldq};
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    return type == ES_FP32 ? run_write<float>(a, st) : type == ES_FP16 ? run_write<_Float16>(a, st) : run_write<__bf16>(a, st);
+}
+
+int es_q8_read(const int8_t* codes, int32_t ldq, const float* scale, int64_t N, int32_t F, const int32_t* rows, int64_t n,
+               void* Y, int32_t type, int32_t ldy, void* stream)
+{
+    const int size = element_bytes(type);
+    if (check_table(N, F, ldq) != ES_OK || !size || n < 0 || n > INT32_MAX || ldy < F || (!rows && n > N)) return ES_ERR_INVALID_ARG;
+    if (n == 0) return ES_OK;
+    if (!Y || misaligned(Y, size) || misaligned(rows, 4) || (N > 0 && bad_table(codes, scale))) return ES_ERR_INVALID_ARG;
+    const Q8Read a = {codes, scale, rows, Y, n, N, F, ldq, ldy};
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    return type == ES_FP32 ? launch_read<float>(a, st) : type == ES_FP16 ? launch_read<_Float16>(a, st) : launch_read<__bf16>(a, st);
+}
+
+int es_spmm_q8(const int32_t* rowptr, const int32_t* colidx, const float* vals, const int8_t* codes, int32_t ldq,
+               const float* scale, float* Y, int64_t N, int64_t nnz, int32_t F, int32_t ldy, int32_t W, int32_t mode,
+               uint64_t seed, int32_t norm, const int32_t* rows, int64_t n_rows, void* stream)
+{
+    const int bad = check_product(N, nnz, F, ldq, ldy, W, mode, norm);
+    if (bad != ES_OK) return bad;
+    if (n_rows < 0 || n_rows > INT32_MAX || (!rows && n_rows != 0 && n_rows != N)) return ES_ERR_INVALID_ARG;
+    if (n_rows == 0) return ES_OK;
+    if (!Y || misaligned(Y, 4) || misaligned(rows, 4)) return ES_ERR_INVALID_ARG;
+    if (N > 0 && (!rowptr || bad_table(codes, scale) || (nnz > 0 && !colidx))) return ES_ERR_INVALID_ARG;
+    Q8Args a = {};
+    a.rowptr = rowptr; a.colidx = colidx; a.vals = vals; a.codes = codes; a.scale = scale; a.rows = rows; a.Y = Y;
+    a.N = N; a.n_rows = n_rows; a.seed = seed; a.F = F; a.ldq = ldq; a.ldy = ldy;
+    a.W = mode == ES_FULL ? INT32_MAX : W; a.mode = mode; a.norm = norm;
+    uint32_t gx;
+    const int64_t chunks = ((int64_t)F + 15) / 16;
+    const int G = chunks >= 16 ? 16 : next_pow2(chunks);
+    const int64_t gy = (chunks + G - 1) / G;
+    if (!grid_of(n_rows, kWavesPerBlock, &gx) || gy > 65535) return ES_ERR_UNSUPPORTED;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+#define ES_Q8(G_) case G_: hipLaunchKernelGGL(es_q8_spmm_kernel<G_>, dim3(gx, (uint32_t)gy), dim3(kBlockThreads), 0, st, a); break;
+    switch (G) { ES_Q8(1) ES_Q8(2) ES_Q8(4) ES_Q8(8) ES_Q8(16) }
+#undef ES_Q8
+    return launched();
+}
+
+int es_spmm_q8_backward_vals(const int32_t* rowptr, const int32_t* colidx, const float* dY, int32_t ldy, const int8_t* codes,
+                             int32_t ldq, const float* scale, float* dvals, int64_t N, int64_t nnz, int32_t F, int32_t W,
+                             int32_t mode, uint64_t seed, int32_t norm, void* stream)
+{
+    const int bad = check_product(N, nnz, F, ldq, ldy, W, mode, norm);
+    if (bad != ES_OK) return bad;
+    if (N == 0 || nnz == 0) return ES_OK;
+    if (!rowptr || !colidx || !dY || !dvals || misaligned(dY, 4) || misaligned(dvals, 4) || bad_table(codes, scale))
+        return ES_ERR_INVALID_ARG;
+    Q8Args a = {};
+    a.rowptr = rowptr; a.colidx = colidx; a.codes = codes; a.scale = scale; a.Y = dvals; a.dY = dY;
+    a.N = a.n_rows = N; a.seed = seed; a.F = F; a.ldq = ldq; a.ldy = ldy;
+    a.W = mode == ES_FULL ? INT32_MAX : W; a.mode = mode; a.norm = norm;
+    uint32_t gx;
+    const int64_t chunks = ((int64_t)F + 15) / 16;
+    const int G = chunks >= 64 ? 64 : next_pow2(chunks);
+    if (!grid_of(N, kWavesPerBlock, &gx)) return ES_ERR_UNSUPPORTED;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+#define ES_Q8(G_) case G_: hipLaunchKernelGGL(es_q8_vals_kernel<G_>, dim3(gx), dim3(kBlockThreads), 0, st, a); break;
+    switch (G) { ES_Q8(1) ES_Q8(2) ES_Q8(4) ES_Q8(8) ES_Q8(16) ES_Q8(32) ES_Q8(64) }
+#undef ES_Q8
+    return launched();
+}
+
+}  // extern "C"
+
+namespace {
+
+// The parts that the rows of X are cut into: enough workgroups for the chip, at least 256 rows each.
+struct GradPlan {
+    int64_t tiles_m, tiles_n, parts, part_rows;
+};
+
+GradPlan plan_grad(int64_t N, int32_t F, int32_t H, size_t workspace_bytes)
+{
+    GradPlan p;
+    p.tiles_m = ((int64_t)F + kGradTile - 1) / kGradTile;
+    p.tiles_n = ((int64_t)H + kGradTile - 1) / kGradTile;
+    p.parts = 1024 / (p.tiles_m * p.tiles_n) + 1;
+    if (p.parts > (N + 255) / 256) p.parts = (N + 255) / 256;
+    const size_t size = (size_t)F * (size_t)H * sizeof(float);
+    if (p.parts < 1 || (p.parts > 1 && workspace_bytes < size * (size_t)p.parts)) p.parts = 1;
+    p.part_rows = (N + p.parts - 1) / p.parts;
+    return p;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t es_q8_weight_grad_workspace_bytes(int64_t N, int32_t F, int32_t H)
+{
+    if (N < 1 || N > INT32_MAX || F < 1 || F > kMaxF || H < 1) return 0;
+    const GradPlan p = plan_grad(N, F, H, SIZE_MAX);
+    return p.parts > 1 ? (size_t)F * (size_t)H * sizeof(float) * (size_t)p.parts : 0;
+}
+
+int es_q8_weight_grad(const int8_t* codes, int32_t ldq, const float* scale, const float* G, int32_t ldg, float* dW,
+                      int32_t ldw, int64_t N, int32_t F, int32_t H, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (check_table(N, F, ldq) != ES_OK || H < 1 || ldg < H || ldw < H) return ES_ERR_INVALID_ARG;
+    if (!dW || misaligned(dW, 4) || misaligned(workspace, 16)) return ES_ERR_INVALID_ARG;
+    if (N > 0 && (!G || misaligned(G, 4) || bad_table(codes, scale))) return ES_ERR_INVALID_ARG;
+    const GradPlan p = plan_grad(N, F, H, workspace ? workspace_bytes : 0);
+    if (p.tiles_m > INT32_MAX || p.tiles_n > 65535 || p.parts > 65535) return ES_ERR_UNSUPPORTED;
+    Q8Grad a = {codes, scale, G, dW, N, F, H, ldq, ldg, ldw, p.part_rows};
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (p.parts > 1) { a.dW = static_cast<float*>(workspace); a.ldw = H; }
+    hipLaunchKernelGGL(es_q8_grad_kernel, dim3((uint32_t)p.tiles_m, (uint32_t)p.tiles_n, (uint32_t)p.parts), dim3(kBlockThreads),
+                       0, st, a);
+    if (launched() != ES_OK || p.parts == 1) return launched();
+    uint32_t grid;
+    if (!grid_of((int64_t)F * H, kBlockThreads, &grid)) return ES_ERR_UNSUPPORTED;
+    hipLaunchKernelGGL(es_q8_grad_join_kernel, dim3(grid), dim3(kBlockThreads), 0, st, a.dW, (int)p.parts, F, H, dW, ldw);
+    return launched();
+}
+
+}  // extern "C"

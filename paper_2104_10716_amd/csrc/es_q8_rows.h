@@ -1,0 +1,257 @@
+// es_q8_rows.h -- rows as int8 codes with one fp32 scale per row: writing them and reading them back.
+//
+//   scale = fp32(max|x| / 127),  code_c = x_c / scale to the nearest integer, ties to even
+//
+// Both directions move each byte once and are bound by memory: a write reads F elements and writes F16 + 4
+// bytes per row (F16: F rounded up to 16), a read the reverse.
+#ifndef ES_SPMM_Q8_ROWS_H
+#define ES_SPMM_Q8_ROWS_H
+
+#include "es_lanes.h"
+
+namespace {
+
+// Four consecutive elements of a dense row at any alignment of the element's own size (one 64- or 128-bit
+// access: the HSA ABI runs the memory pipeline in unaligned-access mode).
+template <class T> struct Quad { typedef T type __attribute__((ext_vector_type(4), aligned(sizeof(T)))); };
+
+template <class T>
+__device__ __forceinline__ void load_quad(const T* p, int left, float (&v)[4])
+{
+    if (left >= 4) {
+        const typename Quad<T>::type q = *reinterpret_cast<const typename Quad<T>::type*>(p);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = (float)q[j];
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = j < left ? (float)p[j] : 0.0f;
+    }
+}
+
+template <class T>
+__device__ __forceinline__ void store_quad(T* p, int left, const float (&v)[4])
+{
+    if (left >= 4) {
+        typename Quad<T>::type q;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) q[j] = (T)v[j];            // to nearest, ties to even
+        *reinterpret_cast<typename Quad<T>::type*>(p) = q;
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (j < left) p[j] = (T)v[j];
+    }
+}
+
+// Scale of a row whose largest magnitude has these bits (as integers, magnitudes order like their values, infinity and
+// NaN above every number).  Below 127 * 2^-126 the scale would be subnormal: such a row is
+// held as zeros.  A row with an infinity or a NaN gets the scale NaN, and reads back as NaN.
+__device__ __forceinline__ float q8_scale(uint32_t bits)
+{
+    if (bits >= 0x7F800000u) return __uint_as_float(0x7FC00000u);
+    const float m = __uint_as_float(bits);
+    return m < 127.0f * 1.17549435e-38f ? 0.0f : fminf(m / 127.0f, 0x1.0204060000000p+121f);   // 127 times the bound is finite
+}
+
+__device__ __forceinline__ float q8_inverse(float scale) { return scale > 0.0f ? 1.0f / scale : 0.0f; }
+
+// The four codes of v as a word.  x * (1 / scale) is within 2e-5 of the quotient, so its nearest integer is the
+// quotient's or, next to a border, a neighbour of it; the remainder x - r * scale is a multiple of the
+// smaller of the operands' last places and below scale in size, so the fused multiply-add has it exactly,
+// and it says whether r is right.
+__device__ __forceinline__ uint32_t q8_codes(const float (&v)[4], float scale, float inv)
+{
+    float r[4], e[4];
+    float worst = 0.0f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        r[j] = rintf(v[j] * inv);
+        e[j] = 2.0f * fmaf(-r[j], scale, v[j]);
+        worst = fmaxf(worst, fabsf(e[j]));
+    }
+    if (worst >= scale) {                                      // a border, or a row held as zeros
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float a = fabsf(e[j]);
+            if (a > scale || (a == scale && ((int)r[j] & 1))) r[j] += copysignf(1.0f, e[j]);
+        }
+    }
+    uint32_t word = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) word |= ((uint32_t)(int)r[j] & 0xFFu) << (8 * j);
+    return scale > 0.0f ? word : 0u;                           // zeros for scale 0 and NaN
+}
+
+enum { Q8_ALL = 0, Q8_SCANNED = 1, Q8_CLAIMED = 2 };           // how the table's rows are named
+
+struct Q8Write {
+    const void* X;
+    const int32_t* rows;
+    int8_t* codes;
+    float* scale;
+    int64_t n, N;
+    int32_t F, ldx, ldq;
+};
+
+// Rows whose index among a call's ids is at most this can be marked in the place of their scale (see below).
+constexpr int64_t kQ8Claims = (1 << 23) - 2;
+constexpr int64_t kQ8Scan = 2048;
+
+// Which table row element i of the call goes to, or -1.  Of equal ids the last one is written:
+// Q8_SCANNED looks through the ids behind i; Q8_CLAIMED finds i + 1 in place of the row's scale
+// (es_q8_claim_kernel).  A scale is 0, NaN or at least 2^-126, none of which has the bits of such a mark, so a
+// reader that comes after the row's writer is not misled.  The whole team agrees.
+template <int MAP, int TEAM>
+__device__ __forceinline__ int64_t q8_target(const Q8Write& a, int64_t i, int t)
+{
+    if (MAP == Q8_ALL) return i;
+    const int32_t row = a.rows[i];
+    if (row < 0 || row >= a.N) return -1;
+    if (MAP == Q8_CLAIMED) {
+        const uint32_t mark = __hip_atomic_load(reinterpret_cast<const uint32_t*>(a.scale) + row, __ATOMIC_RELAXED,
+                                                __HIP_MEMORY_SCOPE_AGENT);
+        return mark == (uint32_t)(i + 1) ? row : -1;
+    }
+    uint32_t later = 0;
+    for (int64_t j = i + 1 + t; j < a.n; j += TEAM) later |= a.rows[j] == row;
+    later = team_reduce<TEAM>(later, [](uint32_t x, uint32_t y) { return x | y; });
+    return later ? -1 : row;
+}
+
+// A team of TEAM lanes holds UR rows in registers, K quads of each per lane.  More rows at a time keep more bytes in flight.
+template <class T, int TEAM, int K, int UR, int MAP>
+__global__ void __launch_bounds__(kBlockThreads) es_q8_write_kernel(const Q8Write a)
+{
+    const int t = threadIdx.x & (TEAM - 1);
+    const int64_t i0 = ((int64_t)blockIdx.x * (kBlockThreads / TEAM) + threadIdx.x / TEAM) * UR;
+    const int f16 = (a.F + 15) & ~15;
+    float v[UR][K][4];
+    int64_t row[UR];
+#pragma unroll
+    for (int u = 0; u < UR; ++u) {
+        row[u] = i0 + u < a.n ? q8_target<MAP, TEAM>(a, i0 + u, t) : -1;
+        const T* x = static_cast<const T*>(a.X) + (row[u] < 0 ? 0 : i0 + u) * (int64_t)a.ldx;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const int c = (k * TEAM + t) * 4;
+            load_quad(x + c, row[u] < 0 ? 0 : a.F - c, v[u][k]);
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < UR; ++u) {
+        uint32_t bits = 0;
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) bits = max(bits, __float_as_uint(v[u][k][j]) & 0x7FFFFFFFu);
+        bits = team_reduce<TEAM>(bits, [](uint32_t x, uint32_t y) { return max(x, y); });
+        if (row[u] < 0) continue;
+        const float scale = q8_scale(bits);
+        const float inv = q8_inverse(scale);
+        int8_t* out = a.codes + row[u] * (int64_t)a.ldq;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const int c = (k * TEAM + t) * 4;
+            if (c < f16) *reinterpret_cast<uint32_t*>(out + c) = q8_codes(v[u][k], scale, inv);
+        }
+        if (t == 0)
+            __hip_atomic_store(reinterpret_cast<uint32_t*>(a.scale) + row[u], __float_as_uint(scale), __ATOMIC_RELAXED,
+                               __HIP_MEMORY_SCOPE_AGENT);
+    }
+}
+
+// Rows too wide for a wave's registers: a workgroup per row reads it twice, the second time from the caches.
+template <class T, int MAP>
+__global__ void __launch_bounds__(kBlockThreads) es_q8_write_wide_kernel(const Q8Write a)
+{
+    __shared__ uint32_t part[kWavesPerBlock];
+    const int64_t i = blockIdx.x;
+    const int lane = threadIdx.x & (kWaveSize - 1), wave = threadIdx.x >> 6;
+    const int64_t row = q8_target<MAP, kWaveSize>(a, i, lane);
+    // every wave has to know before one of them replaces the mark
+    __syncthreads();
+    if (row < 0) return;
+    const T* x = static_cast<const T*>(a.X) + i * (int64_t)a.ldx;
+    const int64_t f16 = ((int64_t)a.F + 15) & ~(int64_t)15;
+    uint32_t bits = 0;
+    float v[4];
+    for (int64_t c = threadIdx.x * 4; c < a.F; c += kBlockThreads * 4) {
+        load_quad(x + c, (int)min((int64_t)4, a.F - c), v);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) bits = max(bits, __float_as_uint(v[j]) & 0x7FFFFFFFu);
+    }
+    bits = team_reduce<kWaveSize>(bits, [](uint32_t p, uint32_t q) { return max(p, q); });
+    if (lane == 0) part[wave] = bits;
+    __syncthreads();
+    for (int w = 0; w < kWavesPerBlock; ++w) bits = max(bits, part[w]);
+    const float scale = q8_scale(bits);
+    const float inv = q8_inverse(scale);
+    int8_t* out = a.codes + row * (int64_t)a.ldq;
+    for (int64_t c = threadIdx.x * 4; c < f16; c += kBlockThreads * 4) {
+        load_quad(x + c, (int)max((int64_t)0, min((int64_t)4, a.F - c)), v);
+        *reinterpret_cast<uint32_t*>(out + c) = q8_codes(v, scale, inv);
+    }
+    if (threadIdx.x == 0)
+        __hip_atomic_store(reinterpret_cast<uint32_t*>(a.scale) + row, __float_as_uint(scale), __ATOMIC_RELAXED,
+                           __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// CLAIM == false: the scales of the rows to be written become 0; true: then the largest i + 1 of the ids i that name the row.
+template <bool CLAIM>
+__global__ void __launch_bounds__(kBlockThreads) es_q8_claim_kernel(const Q8Write a)
+{
+    const int64_t i = (int64_t)blockIdx.x * kBlockThreads + threadIdx.x;
+    if (i >= a.n) return;
+    const int32_t row = a.rows[i];
+    if (row < 0 || row >= a.N) return;
+    uint32_t* mark = reinterpret_cast<uint32_t*>(a.scale) + row;
+    if (CLAIM)
+        __hip_atomic_fetch_max(mark, (uint32_t)(i + 1), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    else
+        __hip_atomic_store(mark, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+struct Q8Read {
+    const int8_t* codes;
+    const float* scale;
+    const int32_t* rows;
+    void* Y;
+    int64_t n, N;
+    int32_t F, ldq, ldy;
+};
+
+// Four codes per lane at a time: the stores, which are most of the bytes, are whole lines.
+template <class T, int TEAM, int UR>
+__global__ void __launch_bounds__(kBlockThreads) es_q8_read_kernel(const Q8Read a)
+{
+    const int t = threadIdx.x & (TEAM - 1);
+    const int64_t i0 = ((int64_t)blockIdx.x * (kBlockThreads / TEAM) + threadIdx.x / TEAM) * UR;
+    int64_t row[UR];
+    float scale[UR];
+#pragma unroll
+    for (int u = 0; u < UR; ++u) {
+        row[u] = i0 + u;
+        if (a.rows && i0 + u < a.n) row[u] = a.rows[i0 + u];
+        if (i0 + u >= a.n || row[u] < 0 || row[u] >= a.N) row[u] = -1;
+    }
+#pragma unroll
+    for (int u = 0; u < UR; ++u) scale[u] = row[u] < 0 ? 0.0f : a.scale[row[u]];
+    for (int64_t c = t * 4; c < a.F; c += TEAM * 4) {
+        uint32_t q[UR];
+#pragma unroll
+        for (int u = 0; u < UR; ++u)
+            q[u] = row[u] < 0 ? 0u : *reinterpret_cast<const uint32_t*>(a.codes + row[u] * (int64_t)a.ldq + c);
+#pragma unroll
+        for (int u = 0; u < UR; ++u) {
+            if (i0 + u >= a.n) continue;
+            float v[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = scale[u] * (float)(int8_t)(q[u] >> (8 * j));
+            store_quad(static_cast<T*>(a.Y) + (i0 + u) * (int64_t)a.ldy + c, (int)min((int64_t)4, a.F - c), v);
+        }
+    }
+}
+
+}  // namespace
+
+#endif  // ES_SPMM_Q8_ROWS_H
