@@ -482,15 +482,25 @@ int es_q8_read(const int8_t* codes, int32_t ldq, const float* scale, int64_t N, 
  *           once (serving: the batch's nodes); an id outside [0, N) gives a row of
  *           zeros.  NULL: all rows, n_rows == N.
  *   Y       n_rows rows of F fp32, row stride ldy >= F, overwritten
- *   nnz     rowptr[N], a launch-shape hint as in es_spmm
- * Accumulation is fp32 in a fixed order: the same call gives the same bits.  A row of
- * the table that no kept entry names has no influence, whatever it holds.
+ *   nnz     rowptr[N]; sizes the workspace: with a smaller number rows may come out
+ *           wrong, though no other memory is touched
+ *   workspace  es_spmm_q8_workspace_bytes(N, nnz, F, W, mode, n_rows) bytes, 16-byte aligned
+ *           (0: none is of use): the sums of pieces of rows that keep very many entries,
+ *           or of a few asked rows, which many workgroups then share.  Contents on entry are
+ *           irrelevant, on return unspecified; calls that share it must be ordered
+ *           (same stream).  With a smaller one, or none, such a row is one workgroup's.
+ * Accumulation is fp32 in an order that the sizes and the workspace fix: the same
+ * call gives the same bits.  A row of the table that no kept entry names has no
+ * influence, whatever it holds.
  */
+size_t es_spmm_q8_workspace_bytes(int64_t N, int64_t nnz, int32_t F, int32_t W, int32_t mode,
+                                  int64_t n_rows);
+
 int es_spmm_q8(const int32_t* rowptr, const int32_t* colidx, const float* vals,
                const int8_t* codes, int32_t ldq, const float* scale, float* Y,
                int64_t N, int64_t nnz, int32_t F, int32_t ldy, int32_t W, int32_t mode,
                uint64_t seed, int32_t norm, const int32_t* rows, int64_t n_rows,
-               void* stream);
+               void* workspace, size_t workspace_bytes, void* stream);
 
 /*
  * es_spmm_q8_backward_vals -- the gradient of the product with respect to `vals`, for

@@ -123,7 +123,10 @@ def load_library():
     lib.es_q8_read.restype = ctypes.c_int
     lib.es_q8_read.argtypes = [vp, i32, vp, i64, i32, vp, i64, vp, i32, i32, vp]
     lib.es_spmm_q8.restype = ctypes.c_int
-    lib.es_spmm_q8.argtypes = [vp, vp, vp, vp, i32, vp, vp, i64, i64, i32, i32, i32, i32, ctypes.c_uint64, i32, vp, i64, vp]
+    lib.es_spmm_q8.argtypes = [vp, vp, vp, vp, i32, vp, vp, i64, i64, i32, i32, i32, i32, ctypes.c_uint64, i32, vp, i64, vp,
+                               size_t, vp]
+    lib.es_spmm_q8_workspace_bytes.restype = size_t
+    lib.es_spmm_q8_workspace_bytes.argtypes = [i64, i64, i32, i32, i32, i64]
     lib.es_spmm_q8_backward_vals.restype = ctypes.c_int
     lib.es_spmm_q8_backward_vals.argtypes = [vp, vp, vp, i32, vp, i32, vp, vp, i64, i64, i32, i32, i32, ctypes.c_uint64,
                                              i32, vp]
@@ -645,6 +648,25 @@ def _checked(rc, where):
         raise EsSpmmError(rc, where)
 
 
+def _workspace(workspace, need, stream):
+    """(workspace, bytes): the caller's, or `need` bytes from torch's allocator in the pool of the stream that will use
+    them: given back when the call returns, they are handed out again in that stream's order only."""
+    import torch
+    if workspace is None:
+        if not need:
+            return None, 0
+        if isinstance(stream, int):
+            stream = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
+        if stream is None:
+            workspace = torch.empty(need, dtype=torch.uint8, device="cuda")
+        else:
+            with torch.cuda.stream(stream):
+                workspace = torch.empty(need, dtype=torch.uint8, device="cuda")
+    elif not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous device tensor")
+    return workspace, workspace.numel() * workspace.element_size()
+
+
 def es_q8_row_bytes(F: int) -> int:
     """Bytes of a row of F codes (F rounded up to 16): a table is
     torch.empty((N, es_q8_row_bytes(F)), dtype=torch.int8) and a float32 scale per row."""
@@ -693,11 +715,18 @@ def _q8_graph(rowptr, colidx, codes, scale, F):
     return N, ldq
 
 
-def es_spmm_q8(rowptr, colidx, vals, codes, scale, Y, W: int, mode, seed: int = 0, norm="none", rows=None, stream=None):
+def es_spmm_q8_workspace_bytes(N: int, nnz: int, F: int, W: int, mode, n_rows: int) -> int:
+    return int(load_library().es_spmm_q8_workspace_bytes(int(N), int(nnz), int(F), int(W), _mode(mode), int(n_rows)))
+
+
+def es_spmm_q8(rowptr, colidx, vals, codes, scale, Y, W: int, mode, seed: int = 0, norm="none", rows=None, workspace=None,
+               stream=None):
     """Y[i] = f * sum of vals[p] * (row colidx[p] of the table) over the kept entries p of row rows[i] (int32 ids
-    in any order; outside [0, N): zeros), or of every row; Y float32 [n, F].  Returns Y."""
+    in any order; outside [0, N): zeros), or of every row; Y float32 [n, F].  `workspace`: a contiguous device
+    tensor of es_spmm_q8_workspace_bytes(N, len(colidx), F, W, mode, n) bytes; by default one from torch's allocator.
+    Returns Y."""
     import torch
-    st = _here(stream, rowptr=rowptr, colidx=colidx, vals=vals, codes=codes, scale=scale, Y=Y, rows=rows)
+    st = _here(stream, rowptr=rowptr, colidx=colidx, vals=vals, codes=codes, scale=scale, Y=Y, rows=rows, workspace=workspace)
     n, F, ldy = _matrix(Y, "Y")
     if F < 1 or Y.dtype != torch.float32:
         raise ValueError("Y must be float32 with at least one column")
@@ -706,10 +735,14 @@ def es_spmm_q8(rowptr, colidx, vals, codes, scale, Y, W: int, mode, seed: int = 
         raise ValueError("Y needs one row per CSR row")
     if vals is not None and (vals.dtype != torch.float32 or vals.numel() != colidx.numel() or not vals.is_contiguous()):
         raise ValueError("vals must be contiguous float32, one per entry of colidx")
-    _checked(load_library().es_spmm_q8(
+    lib = load_library()
+    need = int(lib.es_spmm_q8_workspace_bytes(N, colidx.numel(), F, int(W), _mode(mode), n)) if workspace is None else 0
+    workspace, ws_bytes = _workspace(workspace, need, stream)
+    _checked(lib.es_spmm_q8(
         rowptr.data_ptr() or None, colidx.data_ptr() or None, None if vals is None else vals.data_ptr() or None,
         codes.data_ptr() or None, ldq, scale.data_ptr() or None, Y.data_ptr() or None, N, colidx.numel(), F, ldy, int(W),
-        _mode(mode), int(seed) & 0xFFFFFFFFFFFFFFFF, _norm(norm), _ids(rows, n), n, st), "es_spmm_q8")
+        _mode(mode), int(seed) & 0xFFFFFFFFFFFFFFFF, _norm(norm), _ids(rows, n), n,
+        workspace.data_ptr() if ws_bytes else None, ws_bytes, st), "es_spmm_q8")
     return Y
 
 
@@ -750,25 +783,9 @@ def es_q8_weight_grad(codes, scale, G, dW, workspace=None, stream=None):
     if n != N:
         raise ValueError("G needs one row per row of codes")
     lib = load_library()
-    if workspace is None:
-        need = int(lib.es_q8_weight_grad_workspace_bytes(N, F, H))
-        if need:
-            with torch.cuda.stream(_torch_stream(stream)):
-                workspace = torch.empty(need, dtype=torch.uint8, device=G.device)
-    elif not workspace.is_contiguous():
-        raise ValueError("workspace must be a contiguous device tensor")
-    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    need = int(lib.es_q8_weight_grad_workspace_bytes(N, F, H)) if workspace is None else 0
+    workspace, ws_bytes = _workspace(workspace, need, stream)
     _checked(lib.es_q8_weight_grad(codes.data_ptr() or None, ldq, scale.data_ptr() or None, G.data_ptr() or None, ldg,
                                    dW.data_ptr() or None, ldw, N, F, H, workspace.data_ptr() if ws_bytes else None, ws_bytes,
                                    st), "es_q8_weight_grad")
     return dW
-
-
-def _torch_stream(stream):
-    """A stream of torch for None, an address or a stream, so that memory comes from that stream's pool."""
-    import torch
-    if stream is None:
-        return torch.cuda.current_stream()
-    if isinstance(stream, int):
-        return torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
-    return stream

@@ -115,6 +115,94 @@ int check_product(int64_t N, int64_t nnz, int32_t F, int32_t ldq, int32_t ld, in
     return ES_OK;
 }
 
+// Everything the host decides about one product on 8-bit rows.
+struct Q8Plan {
+    int G, R;                  // lanes per row of codes, rows per wave
+    int64_t slices;            // blocks of 16 G columns
+    bool few;                  // es_q8_few_kernel
+    int32_t splits;            // its pieces per row
+    int32_t long_k, piece;
+    int64_t pieces;            // sums of pieces the workspace holds
+    int64_t nblocks, per_xcd, long_blocks, grid_x;
+};
+
+constexpr int64_t kFewRows = 512;
+
+Q8Plan plan_q8(int64_t N, int64_t nnz, int32_t F, int32_t W, int32_t mode, int64_t n_rows, bool may_split = true)
+{
+    Q8Plan p = {};
+    const int64_t chunks = ((int64_t)F + 15) / 16;
+    p.G = chunks >= 16 ? 16 : next_pow2(chunks);
+    // wide rows: the fewest bytes, of codes and of entries re-read per block of columns
+    if (chunks > 8 && (chunks + 7) / 8 * (8 * 16 + 32) < (chunks + 15) / 16 * (16 * 16 + 32)) p.G = 8;
+    p.slices = (chunks + p.G - 1) / p.G;
+    const int64_t Wk = mode == ES_FULL ? INT32_MAX : W;
+    double mean = N > 0 ? (double)nnz / (double)N : 0.0;
+    if (mean > (double)Wk) mean = (double)Wk;
+    if (mean < 1.0) mean = 1.0;
+
+    p.few = may_split && n_rows <= kFewRows && Wk > 128;
+    if (p.few) {
+        p.splits = (int32_t)(2048 / n_rows);
+        if (p.splits > 64) p.splits = 64;
+        const int64_t most = nnz < Wk ? nnz : Wk;              // no row has more
+        if (p.splits > (most + 127) / 128) p.splits = (int32_t)((most + 127) / 128);
+        if (p.splits < 1) p.splits = 1;
+        p.pieces = p.splits > 1 ? n_rows * p.splits : 0;
+        p.grid_x = n_rows * p.splits;
+        p.piece = p.long_k = INT32_MAX;
+        return p;
+    }
+    // rows per wave: a batch of loads for every lane, but not more slots than a typical row has entries
+    p.R = 1;
+    while (p.R < 4 && (double)(p.R * p.G) * mean < 64.0 * kQ8Batch) p.R *= 2;
+    // a wave retires a batch of E entries per lane in some 1.5 us; a row should not take it a tenth of the launch
+    const double entries = mean * (double)n_rows;
+    const double us = entries * (double)(p.slices * (p.G * 16 + 12)) / 5.0e6;
+    double k = 64.0 / (p.R * p.G) * kQ8Batch * 0.07 * us;
+    if (k < 4.0 * mean) k = 4.0 * mean;
+    p.long_k = k < 128.0 ? 128 : k > 1.0e9 ? 1000000000 : (int32_t)k;
+    int64_t piece = 1024;
+    while (piece * 8192 < nnz) piece *= 2;
+    p.piece = (int32_t)piece;
+    const bool long_rows = Wk > p.long_k;
+    p.pieces = Wk > piece && nnz > piece ? 2 * (nnz / piece + 1) : 0;
+    if (!p.pieces) p.piece = INT32_MAX;
+    p.long_blocks = long_rows ? (n_rows + kQ8ScanRows - 1) / kQ8ScanRows * kQ8Share : 0;
+    p.nblocks = (n_rows + kWavesPerBlock * p.R - 1) / (kWavesPerBlock * p.R);
+    p.per_xcd = (p.nblocks + kNumXcd - 1) / kNumXcd;
+    p.grid_x = p.per_xcd * kNumXcd + p.long_blocks;
+    return p;
+}
+
+template <bool WIDE>
+int launch_q8(const Q8Args& a, const Q8Plan& p, hipStream_t st)
+{
+    const dim3 grid((uint32_t)p.grid_x, (uint32_t)p.slices), block(kBlockThreads);
+    if (p.few) {
+#define ES_Q8(G_) case G_: hipLaunchKernelGGL((es_q8_few_kernel<G_, WIDE>), grid, block, 0, st, a); break;
+        switch (p.G) { ES_Q8(1) ES_Q8(2) ES_Q8(4) ES_Q8(8) ES_Q8(16) }
+#undef ES_Q8
+        if (launched() != ES_OK) return ES_ERR_LAUNCH;
+        if (p.splits > 1) {
+            const uint32_t gy = (uint32_t)(((int64_t)a.F + kBlockThreads - 1) / kBlockThreads);
+            hipLaunchKernelGGL(es_q8_few_join_kernel, dim3((uint32_t)a.n_rows, gy < 64 ? gy : 64), block, 0, st, a);
+        }
+        return launched();
+    }
+#define ES_Q8R(G_, R_) case (G_) * 8 + (R_): hipLaunchKernelGGL((es_q8_spmm_kernel<G_, R_, WIDE>), grid, block, 0, st, a); break;
+#define ES_Q8(G_) ES_Q8R(G_, 1) ES_Q8R(G_, 2) ES_Q8R(G_, 4)
+    switch (p.G * 8 + p.R) { ES_Q8(1) ES_Q8(2) ES_Q8(4) ES_Q8(8) ES_Q8(16) }
+#undef ES_Q8
+#undef ES_Q8R
+    if (launched() != ES_OK) return ES_ERR_LAUNCH;
+    if (p.pieces) {
+        hipLaunchKernelGGL(es_q8_join_kernel, dim3((uint32_t)((a.n_rows + kQ8ScanRows - 1) / kQ8ScanRows)), block, 0, st, a);
+        return launched();
+    }
+    return ES_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -145,30 +233,43 @@ int es_q8_read(const int8_t* codes, int32_t ldq, const float* scale, int64_t N, 
     return type == ES_FP32 ? launch_read<float>(a, st) : type == ES_FP16 ? launch_read<_Float16>(a, st) : launch_read<__bf16>(a, st);
 }
 
+size_t es_spmm_q8_workspace_bytes(int64_t N, int64_t nnz, int32_t F, int32_t W, int32_t mode, int64_t n_rows)
+{
+    if (check_product(N, nnz, F, 16 * (int32_t)(((int64_t)F + 15) / 16), F, W, mode, ES_NORM_NONE) != ES_OK || n_rows < 1 ||
+        n_rows > INT32_MAX)
+        return 0;
+    const Q8Plan p = plan_q8(N, nnz, F, W, mode, n_rows);
+    return (size_t)p.pieces * (size_t)F * sizeof(float);
+}
+
 int es_spmm_q8(const int32_t* rowptr, const int32_t* colidx, const float* vals, const int8_t* codes, int32_t ldq,
                const float* scale, float* Y, int64_t N, int64_t nnz, int32_t F, int32_t ldy, int32_t W, int32_t mode,
-               uint64_t seed, int32_t norm, const int32_t* rows, int64_t n_rows, void* stream)
+               uint64_t seed, int32_t norm, const int32_t* rows, int64_t n_rows, void* workspace, size_t workspace_bytes,
+               void* stream)
 {
     const int bad = check_product(N, nnz, F, ldq, ldy, W, mode, norm);
     if (bad != ES_OK) return bad;
     if (n_rows < 0 || n_rows > INT32_MAX || (!rows && n_rows != 0 && n_rows != N)) return ES_ERR_INVALID_ARG;
     if (n_rows == 0) return ES_OK;
-    if (!Y || misaligned(Y, 4) || misaligned(rows, 4)) return ES_ERR_INVALID_ARG;
+    if (!Y || misaligned(Y, 4) || misaligned(rows, 4) || misaligned(workspace, 16)) return ES_ERR_INVALID_ARG;
     if (N > 0 && (!rowptr || bad_table(codes, scale) || (nnz > 0 && !colidx))) return ES_ERR_INVALID_ARG;
     Q8Args a = {};
     a.rowptr = rowptr; a.colidx = colidx; a.vals = vals; a.codes = codes; a.scale = scale; a.rows = rows; a.Y = Y;
     a.N = N; a.n_rows = n_rows; a.seed = seed; a.F = F; a.ldq = ldq; a.ldy = ldy;
     a.W = mode == ES_FULL ? INT32_MAX : W; a.mode = mode; a.norm = norm;
-    uint32_t gx;
-    const int64_t chunks = ((int64_t)F + 15) / 16;
-    const int G = chunks >= 16 ? 16 : next_pow2(chunks);
-    const int64_t gy = (chunks + G - 1) / G;
-    if (!grid_of(n_rows, kWavesPerBlock, &gx) || gy > 65535) return ES_ERR_UNSUPPORTED;
-    hipStream_t st = static_cast<hipStream_t>(stream);
-#define ES_Q8(G_) case G_: hipLaunchKernelGGL(es_q8_spmm_kernel<G_>, dim3(gx, (uint32_t)gy), dim3(kBlockThreads), 0, st, a); break;
-    switch (G) { ES_Q8(1) ES_Q8(2) ES_Q8(4) ES_Q8(8) ES_Q8(16) }
-#undef ES_Q8
-    return launched();
+    Q8Plan p = plan_q8(N, nnz, F, W, mode, n_rows);
+    if (p.pieces && (!workspace || workspace_bytes < (size_t)p.pieces * (size_t)F * sizeof(float))) {
+        if (p.few) p = plan_q8(N, nnz, F, W, mode, n_rows, false);
+        p.pieces = 0;                                          // a long row is one workgroup's
+        p.piece = INT32_MAX;
+    }
+    const bool wide = (uint64_t)N * (uint64_t)(ldq / kQ8Cols) > 0xFFFFFFFFull;
+    a.row_units = wide ? 0u : (uint32_t)(ldq / kQ8Cols);
+    a.partial = static_cast<float*>(workspace);
+    a.pieces = p.pieces; a.piece = p.piece; a.long_k = p.long_k; a.splits = p.splits;
+    if (p.grid_x > INT32_MAX || p.slices > 65535) return ES_ERR_UNSUPPORTED;
+    a.nblocks = (uint32_t)p.nblocks; a.blocks_per_xcd = (uint32_t)p.per_xcd; a.long_blocks = (uint32_t)p.long_blocks;
+    return wide ? launch_q8<true>(a, p, static_cast<hipStream_t>(stream)) : launch_q8<false>(a, p, static_cast<hipStream_t>(stream));
 }
 
 int es_spmm_q8_backward_vals(const int32_t* rowptr, const int32_t* colidx, const float* dY, int32_t ldy, const int8_t* codes,

@@ -113,9 +113,9 @@ def test_refusals_answer_on_the_host():
     assert write(rows=FAKE, N=0, n=3, codes=None, scale=None) == 0         # every id is outside an empty table
 
     def spmm(rowptr=FAKE, colidx=FAKE, codes=FAKE, ldq=32, scale=FAKE, Y=FAKE, N=4, nnz=9, F=20, ldy=20, W=2, mode=1, norm=0,
-             rows=None, n=4):
-        return lib.es_spmm_q8(rowptr, colidx, None, codes, ldq, scale, Y, N, nnz, F, ldy, W, mode, 0, norm, rows, n,
-                              None)
+             rows=None, n=4, ws=None):
+        return lib.es_spmm_q8(rowptr, colidx, None, codes, ldq, scale, Y, N, nnz, F, ldy, W, mode, 0, norm, rows, n, ws,
+                              0, None)
 
     def grad(rowptr=FAKE, colidx=FAKE, dY=FAKE, codes=FAKE, ldq=32, scale=FAKE, dvals=FAKE, N=4, nnz=9, F=20, ldy=20, W=2,
              mode=1, norm=0):
@@ -125,7 +125,7 @@ def test_refusals_answer_on_the_host():
             dict(ldy=19), dict(W=0), dict(W=0, mode=2), dict(mode=3), dict(mode=-1), dict(norm=5), dict(norm=-1),
             dict(rowptr=None), dict(colidx=None), dict(codes=None), dict(scale=None), dict(codes=ctypes.c_void_p(0x1008)),
             dict(scale=odd))
-    for bad in both + (dict(Y=None), dict(Y=odd), dict(n=3), dict(n=-1), dict(rows=FAKE, n=2 ** 31), dict(rows=odd)):
+    for bad in both + (dict(Y=None), dict(Y=odd), dict(n=3), dict(n=-1), dict(rows=FAKE, n=2 ** 31), dict(rows=odd), dict(ws=odd)):
         assert spmm(**bad) == -1, bad
     for bad in both + (dict(dvals=None), dict(dvals=odd), dict(dY=None), dict(dY=odd)):
         assert grad(**bad) == -1, bad
