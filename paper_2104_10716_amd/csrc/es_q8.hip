@@ -12,6 +12,7 @@
 namespace {
 
 constexpr int32_t kMaxF = INT32_MAX - 15;
+constexpr int kComputeUnits = 256;
 
 int element_bytes(int32_t type) { return type == ES_FP32 ? 4 : type == ES_FP16 || type == ES_BF16 ? 2 : 0; }
 
@@ -117,7 +118,8 @@ int check_product(int64_t N, int64_t nnz, int32_t F, int32_t ldq, int32_t ld, in
 
 // Everything the host decides about one product on 8-bit rows.
 struct Q8Plan {
-    int G, R;                  // lanes per row of codes, rows per wave
+    int G;                     // lanes per row of codes
+    int32_t wave_rows;         // rows a wave takes
     int64_t slices;            // blocks of 16 G columns
     bool few;                  // es_q8_few_kernel
     int32_t splits;            // its pieces per row
@@ -153,15 +155,16 @@ Q8Plan plan_q8(int64_t N, int64_t nnz, int32_t F, int32_t W, int32_t mode, int64
         p.piece = p.long_k = INT32_MAX;
         return p;
     }
-    // rows per wave: a batch of loads for every lane, but not more slots than a typical row has entries
-    p.R = 1;
-    while (p.R < 4 && (double)(p.R * p.G) * mean < 64.0 * kQ8Batch) p.R *= 2;
-    // a wave retires a batch of E entries per lane in some 1.5 us; a row should not take it a tenth of the launch
+    // Rows per wave: the more, the more alike are those that run side by side; but every SIMD wants some waves.
+    const int side = kWaveSize / (p.G < 4 ? 4 : p.G);          // rows side by side
+    p.wave_rows = 64;
+    while (p.wave_rows > side && n_rows / p.wave_rows < 8 * 4 * kComputeUnits) p.wave_rows /= 2;
+    // a lane retires a batch of entries in some 1.5 us; a row should not take it a tenth of the launch
     const double entries = mean * (double)n_rows;
     const double us = entries * (double)(p.slices * (p.G * 16 + 12)) / 5.0e6;
-    double k = 64.0 / (p.R * p.G) * kQ8Batch * 0.07 * us;
+    double k = kQ8Batch * 0.07 * us;
     if (k < 4.0 * mean) k = 4.0 * mean;
-    p.long_k = k < 128.0 ? 128 : k > 1.0e9 ? 1000000000 : (int32_t)k;
+    p.long_k = k < 64.0 ? 64 : k > 1.0e9 ? 1000000000 : (int32_t)k;
     int64_t piece = 1024;
     while (piece * 8192 < nnz) piece *= 2;
     p.piece = (int32_t)piece;
@@ -169,7 +172,7 @@ Q8Plan plan_q8(int64_t N, int64_t nnz, int32_t F, int32_t W, int32_t mode, int64
     p.pieces = Wk > piece && nnz > piece ? 2 * (nnz / piece + 1) : 0;
     if (!p.pieces) p.piece = INT32_MAX;
     p.long_blocks = long_rows ? (n_rows + kQ8ScanRows - 1) / kQ8ScanRows * kQ8Share : 0;
-    p.nblocks = (n_rows + kWavesPerBlock * p.R - 1) / (kWavesPerBlock * p.R);
+    p.nblocks = (n_rows + kWavesPerBlock * p.wave_rows - 1) / (kWavesPerBlock * p.wave_rows);
     p.per_xcd = (p.nblocks + kNumXcd - 1) / kNumXcd;
     p.grid_x = p.per_xcd * kNumXcd + p.long_blocks;
     return p;
@@ -190,11 +193,13 @@ int launch_q8(const Q8Args& a, const Q8Plan& p, hipStream_t st)
         }
         return launched();
     }
-#define ES_Q8R(G_, R_) case (G_) * 8 + (R_): hipLaunchKernelGGL((es_q8_spmm_kernel<G_, R_, WIDE>), grid, block, 0, st, a); break;
-#define ES_Q8(G_) ES_Q8R(G_, 1) ES_Q8R(G_, 2) ES_Q8R(G_, 4)
-    switch (p.G * 8 + p.R) { ES_Q8(1) ES_Q8(2) ES_Q8(4) ES_Q8(8) ES_Q8(16) }
+#define ES_Q8(G_)                                                                                              \
+    case G_:                                                                                                   \
+        if (p.long_blocks) hipLaunchKernelGGL((es_q8_spmm_kernel<G_, true, WIDE>), grid, block, 0, st, a);     \
+        else hipLaunchKernelGGL((es_q8_spmm_kernel<G_, false, WIDE>), grid, block, 0, st, a);                  \
+        break;
+    switch (p.G) { ES_Q8(1) ES_Q8(2) ES_Q8(4) ES_Q8(8) ES_Q8(16) }
 #undef ES_Q8
-#undef ES_Q8R
     if (launched() != ES_OK) return ES_ERR_LAUNCH;
     if (p.pieces) {
         hipLaunchKernelGGL(es_q8_join_kernel, dim3((uint32_t)((a.n_rows + kQ8ScanRows - 1) / kQ8ScanRows)), block, 0, st, a);
@@ -266,7 +271,7 @@ int es_spmm_q8(const int32_t* rowptr, const int32_t* colidx, const float* vals, 
     const bool wide = (uint64_t)N * (uint64_t)(ldq / kQ8Cols) > 0xFFFFFFFFull;
     a.row_units = wide ? 0u : (uint32_t)(ldq / kQ8Cols);
     a.partial = static_cast<float*>(workspace);
-    a.pieces = p.pieces; a.piece = p.piece; a.long_k = p.long_k; a.splits = p.splits;
+    a.pieces = p.pieces; a.piece = p.piece; a.long_k = p.long_k; a.splits = p.splits; a.wave_rows = p.wave_rows;
     if (p.grid_x > INT32_MAX || p.slices > 65535) return ES_ERR_UNSUPPORTED;
     a.nblocks = (uint32_t)p.nblocks; a.blocks_per_xcd = (uint32_t)p.per_xcd; a.long_blocks = (uint32_t)p.long_blocks;
     return wide ? launch_q8<true>(a, p, static_cast<hipStream_t>(stream)) : launch_q8<false>(a, p, static_cast<hipStream_t>(stream));

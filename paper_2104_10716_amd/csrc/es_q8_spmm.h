@@ -5,8 +5,7 @@
 //
 // A lane covers 16 columns, one 128-bit load of codes, and turns them into fp32 with one conversion and
 // one fused multiply-add each; a whole line of 128 codes is gathered by 8 lanes.  G lanes cover a row's
-// columns (blockIdx.y: which ones), R rows share a wave and E = 64 / (R G) entries of a row run side by side.  The weight
-// a_p * scale[c_p] is formed where the entries are staged, one gather for 64 of them.
+// columns (blockIdx.y: which ones).  The weight a_p * scale[c_p] is formed where the entries are staged.
 #ifndef ES_SPMM_Q8_SPMM_H
 #define ES_SPMM_Q8_SPMM_H
 
@@ -17,8 +16,7 @@ namespace {
 
 constexpr int kQ8Cols = 16;                                    // columns of a lane
 constexpr int kQ8Tile = 256;                                   // staged entries per wave
-constexpr int kQ8TileStride = kQ8Tile + 64;                    // and pad slots between the rows' shares
-constexpr int kQ8Batch = 4;                                    // loads of codes in flight per lane
+constexpr int kQ8Batch = 4;                                     // loads of codes in flight per lane
 constexpr int kQ8ScanRows = 1024;                              // rows that a group of long-row workgroups scans
 constexpr int kQ8Share = 16;                                   // workgroups of such a group
 static_assert(kQ8Share % kNumXcd == 0, "long-row workgroups must not shift the XCD phase");
@@ -42,6 +40,7 @@ struct Q8Args {
     int64_t pieces;            // capacity of `partial`
     uint32_t nblocks, blocks_per_xcd, long_blocks;
     int32_t splits;            // es_q8_few_kernel: pieces a row may be cut into
+    int32_t wave_rows;         // rows of a wave, a power of two up to 64
 };
 
 typedef uint32_t uint4_v __attribute__((ext_vector_type(4)));
@@ -83,110 +82,97 @@ __device__ __forceinline__ uint4_v q8_load(const Q8Args& a, const int8_t* codes,
     return *reinterpret_cast<const uint4_v*>(codes + at);
 }
 
-// Slots [0, count) of a tile, lane t of a team of `team`: the codes' place and the weight a_p * scale.
-template <bool WIDE>
-__device__ __forceinline__ void q8_stage(const Q8Args& a, RowSampler& s, int t, int team, int count, int32_t base, uint2* tile)
+// One tile of a row: TEAM lanes stage up to 4 TEAM entries from slot t0 on and multiply the first `most` of them (wave-uniform;
+// no row of the wave has more here) with their rows' columns from `codes` on.  Slots from `count` on add
+// nothing: their weight is 0, codes are finite, and they name a row of the table, that of entry `spare`.  All of a lane's
+// loads of one kind are in flight together.
+template <int G, int TEAM, bool WIDE>
+__device__ __forceinline__ void q8_tile(const Q8Args& a, RowSampler& s, int t, int count, int most, int32_t base, int32_t spare,
+                                        uint2* tile, const int8_t* codes, float (&acc)[kQ8Cols])
 {
-    sample_tile(s, t, team, count, [&](int slot, uint32_t entry) {
-        const int64_t p = (int64_t)base + entry;
-        const int32_t c = a.colidx[p];
-        float w = a.scale[c];
-        if (a.vals) w *= a.vals[p];
-        tile[slot] = make_uint2(q8_key<WIDE>(a, c), __float_as_uint(w));
-    });
-}
-
-// U entries from slot j on, E apart; those from `count` on add nothing: their weight is 0, and codes are finite.
-template <int U, bool WIDE>
-__device__ __forceinline__ void q8_batch(const Q8Args& a, const uint2* tile, int j, int count, int E, const int8_t* codes,
-                                         float (&acc)[kQ8Cols])
-{
-    uint2 ed[U];
-    uint4_v q[U];
+    constexpr int E = TEAM / G, U = kQ8Batch < 4 * G ? kQ8Batch : 4 * G;
+    int64_t p[4];
+    int32_t c[4];
+    float w[4];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const int jj = j + u * E;
-        ed[u] = tile[jj < count ? jj : j];
-        if (jj >= count) ed[u].y = 0u;
+    for (int m = 0; m < 4; ++m) {
+        const uint32_t entry = s.next();
+        p[m] = t + m * TEAM < count ? (int64_t)base + entry : (int64_t)spare;
+        c[m] = a.colidx[p[m]];
+    }
+    if (a.vals) {
+#pragma unroll
+        for (int m = 0; m < 4; ++m) w[m] = a.vals[p[m]];
+    } else {
+#pragma unroll
+        for (int m = 0; m < 4; ++m) w[m] = 1.0f;
     }
 #pragma unroll
-    for (int u = 0; u < U; ++u) q[u] = q8_load<WIDE>(a, codes, ed[u].x);
+    for (int m = 0; m < 4; ++m) {
+        w[m] *= a.scale[c[m]];
+        tile[t + m * TEAM] = make_uint2(q8_key<WIDE>(a, c[m]), t + m * TEAM < count ? __float_as_uint(w[m]) : 0u);
+    }
+    wave_lds_fence();
+
+    // edge slot e has the entries j + e U .. j + e U + U - 1 of each step of U E
+    const uint4_v* pair = reinterpret_cast<const uint4_v*>(tile) + (t / G) * (U / 2);
+#pragma unroll 1
+    for (int j = 0; j < most; j += U * E) {
+        uint4_v q[U];
+        float x[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-        q8_fma(acc, __uint_as_float(ed[u].y), q[u]);
-        __builtin_amdgcn_sched_barrier(0);                     // or every load's codes are converted at once, into registers that spill
+        for (int u = 0; u < U; u += 2) {
+            const uint4_v two = pair[(j + u) / 2];
+            q[u] = q8_load<WIDE>(a, codes, two[0]);
+            q[u + 1] = q8_load<WIDE>(a, codes, two[2]);
+            x[u] = __uint_as_float(two[1]);
+            x[u + 1] = __uint_as_float(two[3]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            q8_fma(acc, x[u], q[u]);
+            __builtin_amdgcn_sched_barrier(0);                 // or every load's codes are converted at once, into registers that spill
+        }
     }
+    wave_lds_fence();
 }
 
-// The staged entries e, e + E, ... < count.  The last batch is the smallest that holds every lane's rest.
-template <bool WIDE>
-__device__ __forceinline__ void q8_consume(const Q8Args& a, const uint2* tile, int count, int e, int E, const int8_t* codes,
-                                           float (&acc)[kQ8Cols])
-{
-    constexpr int U = kQ8Batch;
-    for (int j = e; j < count; j += U * E) {
-        if (__ballot(j + U / 2 * E < count)) q8_batch<U, WIDE>(a, tile, j, count, E, codes, acc);
-        else if (__ballot(j + E < count)) q8_batch<U / 2, WIDE>(a, tile, j, count, E, codes, acc);
-        else q8_batch<1, WIDE>(a, tile, j, count, E, codes, acc);
-    }
-}
-
-// Sums the lanes that are G, 2 G, ... apart inside a team.  Across the halves of a wave and the pairs of its
-// rows of 16 lanes a register swap leaves each side half of the columns, so that what is left to sum
-// halves each time; inside 16 lanes rotations add the rest.  Afterwards acc[0 .. COLS) are this lane's columns from `first` on.
-template <int G, int TEAM>
+// Sums the lanes of a wave that are G, 2 G, ... apart.  Across its halves and the pairs of its rows of 16 lanes a
+// register swap leaves each side half of the columns, so that what is left to sum halves each time; inside 16 lanes
+// rotations add the rest.  Afterwards acc[0 .. 4) are this lane's columns from `first` on.
+template <int G>
 struct Q8Sum {
-    static constexpr int COLS = TEAM == 64 && G <= 16 ? 4 : TEAM == 32 && G <= 16 ? 8 : 16;
-    static_assert(G <= 16 && TEAM >= 16, "a chunk of columns lies inside 16 lanes");
-    __device__ __forceinline__ static int first(int lane)
-    {
-        return TEAM == 64 ? (lane >> 5) * 8 + (lane >> 4 & 1) * 4 : TEAM == 32 ? (lane >> 4 & 1) * 8 : 0;
-    }
+    static constexpr int COLS = 4;
+    static_assert(G <= 16, "a chunk of columns lies inside 16 lanes");
+    __device__ __forceinline__ static int first(int lane) { return (lane >> 5) * 8 + (lane >> 4 & 1) * 4; }
     __device__ __forceinline__ static void run(float (&acc)[kQ8Cols])
     {
-        if constexpr (TEAM == 64) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) { lane_swap<false>(acc[j], acc[j + 8]); acc[j] += acc[j + 8]; }
-        }
-        if constexpr (TEAM >= 32) {
-            constexpr int H = TEAM == 64 ? 4 : 8;
+        for (int j = 0; j < 8; ++j) { lane_swap<false>(acc[j], acc[j + 8]); acc[j] += acc[j + 8]; }
 #pragma unroll
-            for (int j = 0; j < H; ++j) { lane_swap<true>(acc[j], acc[j + H]); acc[j] += acc[j + H]; }
-        }
-        if constexpr (G <= 8) {
+        for (int j = 0; j < 4; ++j) { lane_swap<true>(acc[j], acc[j + 4]); acc[j] += acc[j + 4]; }
 #pragma unroll
-            for (int j = 0; j < COLS; ++j) acc[j] += dpp_move<0x128>(acc[j]);      // row_ror:8
-        }
-        if constexpr (G <= 4) {
-#pragma unroll
-            for (int j = 0; j < COLS; ++j) acc[j] += dpp_move<0x124>(acc[j]);
-        }
-        if constexpr (G <= 2) {
-#pragma unroll
-            for (int j = 0; j < COLS; ++j) acc[j] += dpp_move<0x122>(acc[j]);
-        }
-        if constexpr (G <= 1) {
-#pragma unroll
-            for (int j = 0; j < COLS; ++j) acc[j] += dpp_move<0x121>(acc[j]);
+        for (int j = 0; j < COLS; ++j) {
+            if constexpr (G <= 8) acc[j] += dpp_move<0x128>(acc[j]);               // row_ror:8
+            if constexpr (G <= 4) acc[j] += dpp_move<0x124>(acc[j]);
+            if constexpr (G <= 2) acc[j] += dpp_move<0x122>(acc[j]);
+            if constexpr (G <= 1) acc[j] += dpp_move<0x121>(acc[j]);
         }
     }
 };
 
-// COLS columns from c on into a row of F fp32 at any alignment; what the product writes it does not read again.
-template <int COLS>
-__device__ __forceinline__ void q8_store(float* y, int c, int F, const float (&acc)[kQ8Cols], float f)
+// Columns c .. c + 3 of a row of F fp32 at any alignment; what the product writes it does not read again.
+__device__ __forceinline__ void q8_store(float* y, int c, int F, const float* v, float f)
 {
     typedef float float4_u __attribute__((ext_vector_type(4), aligned(4)));
+    if (c + 4 <= F) {
+        float4_u x = {v[0] * f, v[1] * f, v[2] * f, v[3] * f};
+        __builtin_nontemporal_store(x, reinterpret_cast<float4_u*>(y + c));
+    } else {
 #pragma unroll
-    for (int j = 0; j < COLS; j += 4) {
-        if (c + j + 4 <= F) {
-            float4_u v = {acc[j] * f, acc[j + 1] * f, acc[j + 2] * f, acc[j + 3] * f};
-            __builtin_nontemporal_store(v, reinterpret_cast<float4_u*>(y + c + j));
-        } else {
-#pragma unroll
-            for (int m = 0; m < 4; ++m)
-                if (c + j + m < F) y[c + j + m] = acc[j + m] * f;
-        }
+        for (int m = 0; m < 4; ++m)
+            if (c + m < F) y[c + m] = v[m] * f;
     }
 }
 
@@ -197,24 +183,21 @@ __device__ __forceinline__ void q8_block_sum(const Q8Args& a, const Q8Row& w, in
                                              uint2* lds, float (&acc)[kQ8Cols])
 {
     constexpr int E = kWaveSize / G;
-    using Sum = Q8Sum<G, kWaveSize>;
+    using Sum = Q8Sum<G>;
     const int lane = threadIdx.x & (kWaveSize - 1), wave = threadIdx.x >> 6;
-    uint2* tile = lds + wave * kQ8TileStride;
+    uint2* tile = lds + wave * kQ8Tile;
 #pragma unroll
     for (int j = 0; j < kQ8Cols; ++j) acc[j] = 0.0f;
-    // short pieces are dealt in shares of a batch, so that all four waves have some
+    // short pieces are dealt in smaller shares, so that all four waves have some
     const int step = count >= kWavesPerBlock * kQ8Tile ? kQ8Tile : max(E * kQ8Batch, 64);
     for (int32_t s = wave * step; s < count; s += kWavesPerBlock * step) {
         RowSampler sampler;
         sampler.init(a.mode, a.seed, w.r, (uint32_t)w.n, (uint32_t)a.W, (uint32_t)(t0 + s + lane), kWaveSize);
         const int m = min(count - s, step);
-        q8_stage<WIDE>(a, sampler, lane, kWaveSize, m, w.base, tile);
-        wave_lds_fence();
-        q8_consume<WIDE>(a, tile, m, lane / G, E, codes, acc);
-        wave_lds_fence();
+        q8_tile<G, kWaveSize, WIDE>(a, sampler, lane, m, m, w.base, w.base, tile, codes, acc);
     }
     Sum::run(acc);
-    float* part = reinterpret_cast<float*>(lds + kWavesPerBlock * kQ8TileStride);
+    float* part = reinterpret_cast<float*>(lds + kWavesPerBlock * kQ8Tile);
     __syncthreads();
     if (wave > 0) {
 #pragma unroll
@@ -227,7 +210,7 @@ __device__ __forceinline__ void q8_block_sum(const Q8Args& a, const Q8Row& w, in
             for (int j = 0; j < Sum::COLS; ++j) acc[j] += part[(v * Sum::COLS + j) * kWaveSize + lane];
     }
 }
-constexpr int kQ8Lds = kWavesPerBlock * kQ8TileStride + (kWavesPerBlock - 1) * 4 * kWaveSize / 2;   // tiles and the waves' sums
+constexpr int kQ8Lds = kWavesPerBlock * kQ8Tile + (kWavesPerBlock - 1) * 4 * kWaveSize / 2;   // tiles and the waves' sums
 
 // Place of the piece of a cut row that begins at its slot t0.  Pieces end where the CSR position, base + slot, is a multiple
 // of `piece`; a span of `piece` positions can hold the end of one cut row and the beginning of another.
@@ -300,68 +283,166 @@ __device__ __forceinline__ void q8_piece_slots(const Q8Args& a, const Q8Row& w, 
     count = (int32_t)(hi - lo);
 }
 
-// The product.  The leading workgroups take the long rows, whose waves would run long after the rest of the
-// launch: 16 of them share those among 1024 rows.  The rest take R rows per wave, each XCD a contiguous range of rows.
-template <int G, int R, bool WIDE>
-__global__ void __launch_bounds__(kBlockThreads, 6) es_q8_spmm_kernel(const Q8Args a)
+// What a wave keeps in LDS of each of its rows, in the order in which it takes them.
+struct Q8Kept {
+    int32_t base, n, k, place;                                 // place: among the wave's rows; -1: not this wave's to store
+    uint32_t first, mult;                                      // FastRand: rotation and multiplier of a row that is sampled, else 0
+};
+
+// The rank of lane's k among those of the first `rows` lanes, largest first, ties by lane; the other lanes come behind them.
+__device__ __forceinline__ int q8_rank(int k, int lane, int rows)
 {
-    constexpr int TEAM = kWaveSize / R, E = TEAM / G, T = kQ8Tile / R;
-    __shared__ uint2 lds[kQ8Lds];
-    __shared__ Q8Scan scan;
+    int rank = 0;
+    for (int j0 = 0; j0 < rows; j0 += 4)                       // rows is a multiple of 4
+#pragma unroll
+        for (int j = j0; j < j0 + 4; ++j) {
+            const int other = __builtin_amdgcn_readlane(k, j);
+            rank += (other > k || (other == k && j < lane)) ? 1 : 0;
+        }
+    return lane < rows ? rank : lane;
+}
+
+// The rows [first_row, first_row + wave_rows) of a wave: each lane works out one row, and the rows are put in the order of
+// their kept entries, so that those that run side by side are of about one length.
+__device__ __forceinline__ void q8_plan_rows(const Q8Args& a, int64_t first_row, int lane, Q8Kept* kept)
+{
+    Q8Row w = {-1, 0, 0, 0};
+    if (lane < a.wave_rows) w = q8_row(a, first_row + lane);
+    const bool mine = lane < a.wave_rows && first_row + lane < a.n_rows && w.k <= a.long_k;
+    Q8Kept q = {w.base, w.n, mine ? w.k : 0, mine ? lane : -1, 0u, 0u};
+    if (a.mode == ES_FASTRAND && q.k < w.n) {
+        q.mult = fastrand_multiplier((uint32_t)w.n);
+        q.first = fastrand_offset(a.seed, w.r, (uint32_t)w.n);
+    }
+    kept[q8_rank(q.k, lane, a.wave_rows)] = q;
+    wave_lds_fence();
+}
+
+// Lane t of `team` on a row: the entries of slots t, t + team, ...
+__device__ __forceinline__ void q8_sampler(RowSampler& s, const Q8Kept& w, int t, int team)
+{
+    s.idx = (uint32_t)t;
+    s.step = (uint32_t)team;
+    s.wrap = 0xFFFFFFFFu;
+    if (w.mult) {
+        s.idx = (w.first + (uint32_t)t * w.mult) % (uint32_t)w.n;
+        s.step = ((uint32_t)team * w.mult) % (uint32_t)w.n;
+        s.wrap = (uint32_t)w.n;
+    }
+}
+
+// acc += the lanes of the team (of 4) that hold other entries of the same columns
+template <int G, int TEAM>
+__device__ __forceinline__ void q8_team_sum(float (&acc)[kQ8Cols])
+{
+    static_assert(TEAM == G || (TEAM == 4 && G < 4), "narrow rows: the quad's lanes");
+#pragma unroll
+    for (int j = 0; j < kQ8Cols; ++j) {
+        if constexpr (TEAM > G && G <= 2) acc[j] += dpp_move<0x4E>(acc[j]);        // lanes two apart
+        if constexpr (TEAM > G && G <= 1) acc[j] += dpp_move<0xB1>(acc[j]);        // and one apart
+    }
+}
+
+// The product.  The leading workgroups take the long rows, whose waves would run long after the rest of the
+// launch: 16 of them share those among 1024 rows.  The rest take wave_rows rows per wave, each XCD a contiguous range of
+// rows: TEAM lanes to a row, 64 / TEAM rows side by side, TEAM / G entries of each at once, so that wide rows
+// need no sum across lanes.
+// LONG: there may be long rows (a kernel of its own without them keeps its registers).
+template <int G, bool LONG, bool WIDE>
+__global__ void __launch_bounds__(kBlockThreads, 5) es_q8_spmm_kernel(const Q8Args a)
+{
+    constexpr int TEAM = G < 4 ? 4 : G, ROWS = kWaveSize / TEAM;
+    constexpr int T = 4 * TEAM;                                // entries of a row staged at a time
+    static_assert(T * ROWS == kQ8Tile, "");
+    constexpr int ROW_SLOTS = T + 2;                           // and two of padding: the rows' entry j is in different banks
+    constexpr int WAVE_SLOTS = ROWS * ROW_SLOTS > ROWS * G * kQ8Cols / 2 ? ROWS * ROW_SLOTS : ROWS * G * kQ8Cols / 2;
+    constexpr int SLOTS = !LONG || kWavesPerBlock * WAVE_SLOTS > kQ8Lds ? kWavesPerBlock * WAVE_SLOTS : kQ8Lds;
+    __shared__ __align__(16) uint2 lds[SLOTS];
+    __shared__ union { Q8Kept kept[kWavesPerBlock][kWaveSize]; Q8Scan scan; } sh;
     const int lane = threadIdx.x & (kWaveSize - 1), wave = threadIdx.x >> 6;
     const int l = lane & (G - 1);
     const int c0 = (blockIdx.y * G + l) * kQ8Cols;
     const int8_t* codes = a.codes + (c0 < a.F ? c0 : 0);       // lanes behind the last column load the first ones
     float acc[kQ8Cols];
 
-    if (blockIdx.x < a.long_blocks) {
-        const int64_t first = (int64_t)(blockIdx.x / kQ8Share) * kQ8ScanRows;
-        const int total = q8_scan(a, first, scan);
-        for (int task = (blockIdx.x + blockIdx.x / kQ8Share) % kQ8Share; task < total; task += kQ8Share) {
-            int piece, t0, count;
-            const int64_t i = first + q8_find(scan, task, piece);
-            const Q8Row w = q8_row(a, i);
-            q8_piece_slots(a, w, piece, t0, count);
-            q8_block_sum<G, WIDE>(a, w, t0, count, codes, lds, acc);
-            if (wave == 0 && (lane & 15) < G) {
-                using Sum = Q8Sum<G, kWaveSize>;
-                const int c = c0 + Sum::first(lane);
-                if (w.k <= a.piece) {
-                    q8_store<Sum::COLS>(a.Y + i * (int64_t)a.ldy, c, a.F, acc, row_factor(a.norm, w.n, w.k));
-                } else {
-                    const int64_t at = q8_piece(a, w, t0);
-                    if (at < a.pieces) q8_store<Sum::COLS>(a.partial + at * a.F, c, a.F, acc, 1.0f);
+    if constexpr (LONG) {
+        if (blockIdx.x < a.long_blocks) {
+            const int64_t first = (int64_t)(blockIdx.x / kQ8Share) * kQ8ScanRows;
+            const int total = q8_scan(a, first, sh.scan);
+            for (int task = (blockIdx.x + blockIdx.x / kQ8Share) % kQ8Share; task < total; task += kQ8Share) {
+                int piece, t0, count;
+                const int64_t i = first + q8_find(sh.scan, task, piece);
+                const Q8Row w = q8_row(a, i);
+                q8_piece_slots(a, w, piece, t0, count);
+                q8_block_sum<G, WIDE>(a, w, t0, count, codes, lds, acc);
+                if (wave == 0 && (lane & 15) < G) {
+                    const int c = c0 + Q8Sum<G>::first(lane);
+                    if (w.k <= a.piece) {
+                        q8_store(a.Y + i * (int64_t)a.ldy, c, a.F, acc, row_factor(a.norm, w.n, w.k));
+                    } else {
+                        const int64_t at = q8_piece(a, w, t0);
+                        if (at < a.pieces) q8_store(a.partial + at * a.F, c, a.F, acc, 1.0f);
+                    }
                 }
+                __syncthreads();
             }
-            __syncthreads();
+            return;
         }
-        return;
     }
     const uint32_t b = blockIdx.x - a.long_blocks;
     const uint32_t vb = (b % kNumXcd) * a.blocks_per_xcd + b / kNumXcd;
     if (vb >= a.nblocks) return;
 
-    const int rs = lane / TEAM, t = lane & (TEAM - 1), e = t / G;
-    uint2* tile = lds + wave * kQ8TileStride + rs * (T + E);   // the rows' slots j .. j + E - 1 miss each other's banks
-    const int64_t i = ((int64_t)vb * kWavesPerBlock + wave) * R + rs;
-    const Q8Row w = q8_row(a, i);
-    const bool is_long = w.k > a.long_k;
-    const int k = is_long ? 0 : w.k;
-    RowSampler s;
-    s.init(a.mode, a.seed, w.r, (uint32_t)w.n, (uint32_t)a.W, (uint32_t)t, TEAM);
+    const int64_t first_row = ((int64_t)vb * kWavesPerBlock + wave) * a.wave_rows;
+    Q8Kept* kept = sh.kept[wave];
+    q8_plan_rows(a, first_row, lane, kept);
+    const int rs = lane / TEAM, t = lane & (TEAM - 1);
+    uint2* own = lds + wave * WAVE_SLOTS;
+    uint2* tile = own + rs * ROW_SLOTS;
+    for (int p = rs; p < a.wave_rows; p += ROWS) {
+        const Q8Kept w = kept[p];
+        RowSampler s;
+        q8_sampler(s, w, t, TEAM);
 #pragma unroll
-    for (int j = 0; j < kQ8Cols; ++j) acc[j] = 0.0f;
-    for (int t0 = 0; t0 < k; t0 += T) {
-        const int count = min(k - t0, T);
-        q8_stage<WIDE>(a, s, t, TEAM, count, w.base, tile);
+        for (int j = 0; j < kQ8Cols; ++j) acc[j] = 0.0f;
+        // the first of the rows side by side keeps the most
+        const int most = __builtin_amdgcn_readfirstlane(w.k), spare = __builtin_amdgcn_readfirstlane(w.base);
+        for (int t0 = 0; t0 < most; t0 += T)
+            q8_tile<G, TEAM, WIDE>(a, s, t, w.k - t0, min(most - t0, T), w.base, spare, tile, codes, acc);
+        q8_team_sum<G, TEAM>(acc);
+        // through LDS, so that a store instruction writes whole lines: lane t has the row's quads t, t + TEAM, ...
+        float* out = reinterpret_cast<float*>(own) + rs * (G * kQ8Cols);
+        if (t < G) {
+#pragma unroll
+            for (int j = 0; j < kQ8Cols; j += 4)
+                *reinterpret_cast<float4*>(out + l * kQ8Cols + j) = make_float4(acc[j], acc[j + 1], acc[j + 2], acc[j + 3]);
+        }
         wave_lds_fence();
-        q8_consume<WIDE>(a, tile, count, e, E, codes, acc);
+        const float f = row_factor(a.norm, w.n, w.k);
+#pragma unroll
+        for (int q = 0; q < 4 * G; q += TEAM) {
+            const float4 v = *reinterpret_cast<const float4*>(out + (q + t) * 4);
+            const float v4[4] = {v.x, v.y, v.z, v.w};
+            if (w.place >= 0)
+                q8_store(a.Y + (first_row + w.place) * (int64_t)a.ldy, blockIdx.y * G * kQ8Cols + (q + t) * 4, a.F, v4, f);
+        }
         wave_lds_fence();
     }
-    using Sum = Q8Sum<G, TEAM>;
-    Sum::run(acc);
-    if (i < a.n_rows && !is_long && (t & 15) < G)
-        q8_store<Sum::COLS>(a.Y + i * (int64_t)a.ldy, c0 + Sum::first(lane), a.F, acc, row_factor(a.norm, w.n, w.k));
+}
+
+// The sum of `pieces` numbers in their order, eight of which are requested at a time.
+template <class Get>
+__device__ __forceinline__ float q8_sum_pieces(int pieces, Get&& get)
+{
+    float s = 0.0f;
+    for (int p = 0; p < pieces; p += 8) {
+        float v[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) v[u] = get(min(p + u, pieces - 1));
+#pragma unroll
+        for (int u = 0; u < 8; ++u) s += p + u < pieces ? v[u] : 0.0f;
+    }
+    return s;
 }
 
 // Rows that were cut: the sum of their pieces in order, times the factor.
@@ -382,11 +463,10 @@ __global__ void __launch_bounds__(kBlockThreads) es_q8_join_kernel(const Q8Args 
         const int64_t span = w.base / a.piece;
         const int pieces = q8_pieces(a, w);
         for (int c = threadIdx.x; c < a.F; c += kBlockThreads) {
-            float s = 0.0f;
-            for (int p = 0; p < pieces; ++p) {
+            const float s = q8_sum_pieces(pieces, [&](int p) {
                 const int64_t at = 2 * (span + p) + (p == 0 ? 1 : 0);
-                if (at < a.pieces) s += a.partial[at * a.F + c];
-            }
+                return at < a.pieces ? a.partial[at * a.F + c] : 0.0f;
+            });
             a.Y[i * (int64_t)a.ldy + c] = s * f;
         }
     }
@@ -402,7 +482,7 @@ __device__ __forceinline__ int32_t q8_few_length(const Q8Args& a, int32_t k)
 template <int G, bool WIDE>
 __global__ void __launch_bounds__(kBlockThreads) es_q8_few_kernel(const Q8Args a)
 {
-    using Sum = Q8Sum<G, kWaveSize>;
+    using Sum = Q8Sum<G>;
     __shared__ uint2 lds[kQ8Lds];
     const int lane = threadIdx.x & (kWaveSize - 1), wave = threadIdx.x >> 6;
     const int c0 = (blockIdx.y * G + (lane & (G - 1))) * kQ8Cols;
@@ -417,8 +497,8 @@ __global__ void __launch_bounds__(kBlockThreads) es_q8_few_kernel(const Q8Args a
     q8_block_sum<G, WIDE>(a, w, (int32_t)t0, (int32_t)min((int64_t)length, w.k - t0), codes, lds, acc);
     if (wave == 0 && (lane & 15) < G) {
         const int c = c0 + Sum::first(lane);
-        if (w.k <= length) q8_store<Sum::COLS>(a.Y + i * (int64_t)a.ldy, c, a.F, acc, row_factor(a.norm, w.n, w.k));
-        else q8_store<Sum::COLS>(a.partial + (i * a.splits + piece) * a.F, c, a.F, acc, 1.0f);
+        if (w.k <= length) q8_store(a.Y + i * (int64_t)a.ldy, c, a.F, acc, row_factor(a.norm, w.n, w.k));
+        else q8_store(a.partial + (i * a.splits + piece) * a.F, c, a.F, acc, 1.0f);
     }
 }
 
@@ -431,8 +511,7 @@ __global__ void __launch_bounds__(kBlockThreads) es_q8_few_join_kernel(const Q8A
     const float f = row_factor(a.norm, w.n, w.k);
     const int pieces = (w.k - 1) / length + 1;
     for (int c = blockIdx.y * kBlockThreads + threadIdx.x; c < a.F; c += gridDim.y * kBlockThreads) {
-        float s = 0.0f;
-        for (int p = 0; p < pieces; ++p) s += a.partial[(i * a.splits + p) * a.F + c];
+        const float s = q8_sum_pieces(pieces, [&](int p) { return a.partial[(i * a.splits + p) * a.F + c]; });
         a.Y[i * (int64_t)a.ldy + c] = s * f;
     }
 }
