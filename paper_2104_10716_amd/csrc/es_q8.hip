@@ -305,21 +305,23 @@ int es_spmm_q8_backward_vals(const int32_t* rowptr, const int32_t* colidx, const
 
 namespace {
 
-// The parts that the rows of X are cut into: enough workgroups for the chip, at least 256 rows each.
+// The parts that the rows of X are cut into: two workgroups per compute unit in all, and four steps of each wave or more.
 struct GradPlan {
-    int64_t tiles_m, tiles_n, parts, part_rows;
+    int64_t tiles_m, tiles, parts, part_rows;
 };
 
 GradPlan plan_grad(int64_t N, int32_t F, int32_t H, size_t workspace_bytes)
 {
     GradPlan p;
-    p.tiles_m = ((int64_t)F + kGradTile - 1) / kGradTile;
-    p.tiles_n = ((int64_t)H + kGradTile - 1) / kGradTile;
-    p.parts = 1024 / (p.tiles_m * p.tiles_n) + 1;
-    if (p.parts > (N + 255) / 256) p.parts = (N + 255) / 256;
+    p.tiles_m = ((int64_t)F + kGradM - 1) / kGradM;
+    p.tiles = p.tiles_m * (((int64_t)H + kGradN - 1) / kGradN);
+    p.parts = 2 * kComputeUnits / p.tiles;
+    if (p.parts > N / (4 * kGradRows)) p.parts = N / (4 * kGradRows);
+    if (p.parts > kNumXcd) p.parts -= p.parts % kNumXcd;       // each XCD as many
     const size_t size = (size_t)F * (size_t)H * sizeof(float);
-    if (p.parts < 1 || (p.parts > 1 && workspace_bytes < size * (size_t)p.parts)) p.parts = 1;
-    p.part_rows = (N + p.parts - 1) / p.parts;
+    if (p.parts < 1 || workspace_bytes < size * (size_t)p.parts) p.parts = 1;
+    p.part_rows = ((N + p.parts - 1) / p.parts + kGradRows - 1) / kGradRows * kGradRows;
+    p.parts = p.part_rows ? (N + p.part_rows - 1) / p.part_rows : 1;
     return p;
 }
 
@@ -341,16 +343,20 @@ int es_q8_weight_grad(const int8_t* codes, int32_t ldq, const float* scale, cons
     if (!dW || misaligned(dW, 4) || misaligned(workspace, 16)) return ES_ERR_INVALID_ARG;
     if (N > 0 && (!G || misaligned(G, 4) || bad_table(codes, scale))) return ES_ERR_INVALID_ARG;
     const GradPlan p = plan_grad(N, F, H, workspace ? workspace_bytes : 0);
-    if (p.tiles_m > INT32_MAX || p.tiles_n > 65535 || p.parts > 65535) return ES_ERR_UNSUPPORTED;
-    Q8Grad a = {codes, scale, G, dW, N, F, H, ldq, ldg, ldw, p.part_rows};
+    if (ldq >= 1 << 27 || ldg >= 1 << 27) return ES_ERR_UNSUPPORTED;  // a lane's offset inside 8 rows is held in 32 bits
+    const int64_t grid = (p.parts < kNumXcd ? p.parts : (p.parts + kNumXcd - 1) / kNumXcd * kNumXcd) * p.tiles;
+    if (grid > INT32_MAX) return ES_ERR_UNSUPPORTED;
+    const bool join = p.parts > 1;
+    const Q8Grad a = {codes, scale, G, join ? static_cast<float*>(workspace) : dW, N, F, H, ldq, ldg, join ? H : ldw,
+                      (int32_t)p.tiles_m, (int32_t)p.tiles, p.part_rows, (int32_t)p.parts};
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if (p.parts > 1) { a.dW = static_cast<float*>(workspace); a.ldw = H; }
-    hipLaunchKernelGGL(es_q8_grad_kernel, dim3((uint32_t)p.tiles_m, (uint32_t)p.tiles_n, (uint32_t)p.parts), dim3(kBlockThreads),
-                       0, st, a);
-    if (launched() != ES_OK || p.parts == 1) return launched();
-    uint32_t grid;
-    if (!grid_of((int64_t)F * H, kBlockThreads, &grid)) return ES_ERR_UNSUPPORTED;
-    hipLaunchKernelGGL(es_q8_grad_join_kernel, dim3(grid), dim3(kBlockThreads), 0, st, a.dW, (int)p.parts, F, H, dW, ldw);
+    if (H == 1) hipLaunchKernelGGL(es_q8_grad_kernel<true>, dim3((uint32_t)grid), dim3(kBlockThreads), 0, st, a);
+    else hipLaunchKernelGGL(es_q8_grad_kernel<false>, dim3((uint32_t)grid), dim3(kBlockThreads), 0, st, a);
+    if (launched() != ES_OK) return ES_ERR_LAUNCH;
+    if (!join) return ES_OK;
+    uint32_t gj;
+    if (!grid_of((int64_t)F * H, kWaveSize, &gj)) return ES_ERR_UNSUPPORTED;
+    hipLaunchKernelGGL(es_q8_grad_join_kernel, dim3(gj), dim3(kGradJoin * kWaveSize), 0, st, a.dW, (int)p.parts, F, H, dW, ldw);
     return launched();
 }
 

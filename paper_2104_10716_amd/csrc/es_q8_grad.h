@@ -1,4 +1,15 @@
 // es_q8_grad.h -- dW = X^T G with X held as 8-bit rows: the weight gradient of a dense layer from its input's checkpoint.
+//
+//   dW[i, j] = sum over r of code[r, i] * (scale[r] * G[r, j])
+//
+// On the matrix cores in bf16, exactly: a code has 8 significant bits and is a bf16 number; g = scale * G, rounded once to
+// fp32, is the sum of three bf16 numbers, its leading, middle and last 8 bits (as long as the last are no subnormals, from
+// |g| of 2^-102 on); every product of the two is exact in fp32.  What is rounded is g and the sums, in fp32.
+//
+// A matrix instruction wants 8 rows r of one column i (or j) in a lane's registers, and in memory a row's columns lie
+// side by side.  No data has to be turned for that: a lane loads the same 4 columns of codes (2 of G) of 8 rows, and
+// registers number c of those loads are what the lane owes the c-th of 4 (2) tiles; which 32 columns
+// a tile then has, every fourth (second), is of no consequence until the result is stored.
 #ifndef ES_SPMM_Q8_GRAD_H
 #define ES_SPMM_Q8_GRAD_H
 
@@ -13,53 +24,206 @@ struct Q8Grad {
     float* dW;                 // the result, or the parts' sums
     int64_t N;
     int32_t F, H, ldq, ldg, ldw;
+    int32_t tiles_m, tiles;    // tiles of dW: along F, and in all
     int64_t part_rows;         // rows of X that one part sums
+    int32_t parts;
 };
 
-constexpr int kGradTile = 64;                                  // rows and columns of dW per workgroup
-constexpr int kGradStep = 16;                                  // rows of X staged at a time
+constexpr int kGradM = 128, kGradN = 64;                       // a wave's tile of dW: 4 x 2 tiles of the instruction
+constexpr int kGradStep = 16;                                  // rows of X that an instruction sums
+constexpr int kGradRows = kGradStep * kWavesPerBlock;          // ... and a workgroup's four waves together
 
-// A workgroup sums a 64 x 64 tile of dW over its part's rows, 4 x 4 elements per thread.
-__global__ void __launch_bounds__(kBlockThreads) es_q8_grad_kernel(const Q8Grad a)
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float float2_u __attribute__((ext_vector_type(2), aligned(4)));
+typedef float float4_u4 __attribute__((ext_vector_type(4), aligned(4)));
+
+// What a lane loads of 8 rows.
+struct GradRows {
+    uint32_t code[8];
+    float2_u g[8];
+    float4_u4 scale[2];
+};
+
+// the upper halves of two words: numbers cut to bf16
+__device__ __forceinline__ uint32_t upper_halves(float low, float high)
 {
-    __shared__ float xs[kGradStep][kGradTile], gs[kGradStep][kGradTile];
-    const int tid = threadIdx.x;
-    const int m0 = blockIdx.x * kGradTile, n0 = blockIdx.y * kGradTile;
-    const int64_t lo = blockIdx.z * a.part_rows, hi = min(a.N, lo + a.part_rows);
-    const int tm = (tid / 16) * 4, tn = (tid % 16) * 4;
-    float acc[4][4] = {};
-    for (int64_t r0 = lo; r0 < hi; r0 += kGradStep) {
-        for (int q = tid; q < kGradStep * kGradTile; q += kBlockThreads) {
-            const int i = q / kGradTile, c = q % kGradTile;
-            const int64_t r = r0 + i;
-            xs[i][c] = r < hi && m0 + c < a.F ? (float)a.codes[r * a.ldq + m0 + c] * a.scale[r] : 0.0f;
-            gs[i][c] = r < hi && n0 + c < a.H ? a.G[r * a.ldg + n0 + c] : 0.0f;
+    return __builtin_amdgcn_perm(__float_as_uint(high), __float_as_uint(low), 0x07060302u);
+}
+union GradFrag { uint32_t w[4]; bf16x8 v; };
+
+// The four waves of a workgroup take the part's steps in turn and add up their tiles in LDS, in their order.
+// SINGLE: G has one column, and so no pairs.
+template <bool SINGLE>
+__global__ void __launch_bounds__(kBlockThreads, 2) es_q8_grad_kernel(const Q8Grad a)
+{
+    __shared__ float sums[2][kGradM * kGradN];
+    const int lane = threadIdx.x & (kWaveSize - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n = lane & 31, half = lane >> 5;
+    // the tiles of a part run on one XCD: they read the same rows
+    const uint32_t groups = a.parts < kNumXcd ? 1 : kNumXcd;
+    const uint32_t i = blockIdx.x / groups;
+    const int32_t part = (int32_t)(i / a.tiles * groups + blockIdx.x % groups), tile = (int32_t)(i % a.tiles);
+    if (part >= a.parts) return;
+    const int32_t m0 = tile % a.tiles_m * kGradM, n0 = tile / a.tiles_m * kGradN;
+    const int64_t lo = part * a.part_rows, hi = min(a.N, lo + a.part_rows);
+    const int32_t cm = m0 + 4 * n, cn = n0 + 2 * n;
+    // Lanes behind the last column load the first ones; what they sum is not stored.  Bytes from the step's first row on:
+    const uint32_t at_code = 8u * half * a.ldq + (cm < ((a.F + 15) & ~15) ? cm : 0);
+    const uint32_t at_g = 4u * (8u * half * a.ldg + (cn + 2 <= a.H ? cn : !SINGLE && cn < a.H ? a.H - 2 : 0));
+    const bool last = !SINGLE && cn + 1 == a.H;                // the pair ends with this lane's first column: its second sum
+
+    f32x16 acc[4][2];
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) acc[t][s][j] = 0.0f;
+
+    // Addresses: those of the wave's rows, in scalar registers, and the lane's 32-bit offset.
+    auto load = [&](GradRows& q, int64_t r0) {
+        const char* code = reinterpret_cast<const char*>(a.codes) + r0 * a.ldq;
+        const char* g = reinterpret_cast<const char*>(a.G) + r0 * a.ldg * 4;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) q.scale[j] = *reinterpret_cast<const float4_u4*>(a.scale + r0 + 4 * j + 8u * half);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            q.code[j] = *reinterpret_cast<const uint32_t*>(code + (int64_t)j * a.ldq + at_code);
+            const char* p = g + (int64_t)j * a.ldg * 4 + at_g;
+            if constexpr (SINGLE) { q.g[j].x = *reinterpret_cast<const float*>(p); q.g[j].y = 0.0f; }
+            else q.g[j] = *reinterpret_cast<const float2_u*>(p);
+        }
+    };
+    auto load_end = [&](GradRows& q, int64_t r0) {             // fewer than 16 rows: zeros behind them
+        const int left = (int)(hi - r0) - 8 * half;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            q.code[j] = 0u;
+            q.scale[j / 4][j % 4] = q.g[j].x = q.g[j].y = 0.0f;
+            if (j < left) {
+                const int64_t r = r0 + 8 * half + j;
+                q.code[j] = *reinterpret_cast<const uint32_t*>(a.codes + (r0 + j) * a.ldq + at_code);
+                q.scale[j / 4][j % 4] = a.scale[r];
+                const float* p = reinterpret_cast<const float*>(reinterpret_cast<const char*>(a.G + (r0 + j) * a.ldg) + at_g);
+                q.g[j].x = p[0];
+                if constexpr (!SINGLE) q.g[j].y = p[1];
+            }
+        }
+    };
+    auto multiply = [&](GradRows& q) {
+        // what is loaded is first looked at here: the conversions stay behind the next step's loads
+#pragma unroll
+        for (int j = 0; j < 8; ++j) asm volatile("" : "+v"(q.code[j]), "+v"(q.g[j].x), "+v"(q.g[j].y));
+#pragma unroll
+        for (int j = 0; j < 8; ++j) asm volatile("" : "+v"(q.scale[j / 4][j % 4]));
+        GradFrag x[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int j = 0; j < 8; j += 2)
+                x[t].w[j / 2] = upper_halves((float)(int8_t)(q.code[j] >> (8 * t)), (float)(int8_t)(q.code[j + 1] >> (8 * t)));
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            GradFrag y[3];
+#pragma unroll
+            for (int j = 0; j < 8; j += 2) {
+                float v[2];
+#pragma unroll
+                for (int u = 0; u < 2; ++u) v[u] = (s == 0 ? q.g[j + u].x : q.g[j + u].y) * q.scale[(j + u) / 4][(j + u) % 4];
+#pragma unroll
+                for (int p = 0; p < 3; ++p) {
+                    y[p].w[j / 2] = upper_halves(v[0], v[1]);
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) v[u] -= __uint_as_float(__float_as_uint(v[u]) & 0xFFFF0000u);
+                }
+            }
+#pragma unroll
+            for (int p = 0; p < 3; ++p)
+#pragma unroll
+                for (int t = 0; t < 4; ++t) acc[t][s] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[t].v, y[p].v, acc[t][s], 0, 0, 0);
+        }
+    };
+
+    GradRows q;
+    const int64_t first = lo + wave * kGradStep, full = hi - first >= kGradStep ? (hi - first - kGradStep) / kGradRows + 1 : 0;
+    if (full > 0) {
+        load(q, first);
+        for (int64_t s = 0; s < full; s += 2) {                // the next step's rows are requested before this one's are used
+            GradRows next;
+            load(next, first + min(s + 1, full - 1) * kGradRows);
+            multiply(q);
+            load(q, first + min(s + 2, full - 1) * kGradRows);
+            if (s + 1 < full) multiply(next);
+        }
+    }
+    if (first + full * kGradRows < hi) {
+        load_end(q, first + full * kGradRows);
+        multiply(q);
+    }
+
+    // ((wave 0 + wave 2) + (wave 1 + wave 3))
+#pragma unroll
+    for (int round = 2; round >= 1; --round) {
+        if (wave >= round && wave < 2 * round) {
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int s = 0; s < 2; ++s)
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) sums[wave - round][((t * 2 + s) * 16 + j) * kWaveSize + lane] = acc[t][s][j];
         }
         __syncthreads();
+        if (wave < round) {
 #pragma unroll
-        for (int i = 0; i < kGradStep; ++i)
+            for (int t = 0; t < 4; ++t)
 #pragma unroll
-            for (int m = 0; m < 4; ++m)
+                for (int s = 0; s < 2; ++s)
 #pragma unroll
-                for (int n = 0; n < 4; ++n) acc[m][n] = fmaf(xs[i][tm + m], gs[i][tn + n], acc[m][n]);
+                    for (int j = 0; j < 16; ++j) acc[t][s][j] += sums[wave][((t * 2 + s) * 16 + j) * kWaveSize + lane];
+        }
         __syncthreads();
     }
-    float* out = a.dW + blockIdx.z * ((int64_t)a.F * a.ldw);
+    if (wave > 0) return;
+    float* out = a.dW + part * ((int64_t)a.F * a.ldw);
 #pragma unroll
-    for (int m = 0; m < 4; ++m)
+    for (int t = 0; t < 4; ++t)
 #pragma unroll
-        for (int n = 0; n < 4; ++n)
-            if (m0 + tm + m < a.F && n0 + tn + n < a.H) out[(int64_t)(m0 + tm + m) * a.ldw + n0 + tn + n] = acc[m][n];
+        for (int j = 0; j < 16; ++j) {
+            const int32_t f = m0 + 4 * (8 * (j / 4) + 4 * half + j % 4) + t;
+            if (f >= a.F) continue;
+            float* p = out + (int64_t)f * a.ldw + cn;
+            if (cn + 1 < a.H) {
+                float2_u v = {acc[t][0][j], acc[t][1][j]};
+                *reinterpret_cast<float2_u*>(p) = v;
+            } else if (cn < a.H) {
+                p[0] = last ? acc[t][1][j] : acc[t][0][j];
+            }
+        }
 }
 
-// dW = the sum of the parts, in their order.
-__global__ void __launch_bounds__(kBlockThreads)
+constexpr int kGradJoin = 16;                                  // waves that share 64 elements of dW
+
+// dW = the sum of the parts: wave w adds parts w, w + 16, ..., eight of which are requested at a time, and the waves' sums are
+// added in their order.
+__global__ void __launch_bounds__(kGradJoin * kWaveSize)
 es_q8_grad_join_kernel(const float* __restrict__ part, int parts, int32_t F, int32_t H, float* __restrict__ dW, int32_t ldw)
 {
-    const int64_t i = (int64_t)blockIdx.x * kBlockThreads + threadIdx.x, size = (int64_t)F * H;
-    if (i >= size) return;
+    __shared__ float sums[kGradJoin][kWaveSize];
+    const int lane = threadIdx.x & (kWaveSize - 1), wave = threadIdx.x >> 6;
+    const int64_t size = (int64_t)F * H, i = (int64_t)blockIdx.x * kWaveSize + lane, at = min(i, size - 1);
     float s = 0.0f;
-    for (int p = 0; p < parts; ++p) s += part[p * size + i];
+    for (int p = wave; p < parts; p += 8 * kGradJoin) {
+        float v[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) v[u] = part[min(p + u * kGradJoin, parts - 1) * size + at];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) s += p + u * kGradJoin < parts ? v[u] : 0.0f;
+    }
+    sums[wave][lane] = s;
+    __syncthreads();
+    if (wave > 0 || i >= size) return;
+    for (int w = 1; w < kGradJoin; ++w) s += sums[w][lane];
     dW[i / H * ldw + i % H] = s;
 }
 
