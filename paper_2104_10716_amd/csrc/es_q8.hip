@@ -318,10 +318,13 @@ GradPlan plan_grad(int64_t N, int32_t F, int32_t H, size_t workspace_bytes)
     p.parts = 2 * kComputeUnits / p.tiles;
     if (p.parts > N / (4 * kGradRows)) p.parts = N / (4 * kGradRows);
     if (p.parts > kNumXcd) p.parts -= p.parts % kNumXcd;       // each XCD as many
-    const size_t size = (size_t)F * (size_t)H * sizeof(float);
-    if (p.parts < 1 || workspace_bytes < size * (size_t)p.parts) p.parts = 1;
+    if (p.parts < 1) p.parts = 1;
     p.part_rows = ((N + p.parts - 1) / p.parts + kGradRows - 1) / kGradRows * kGradRows;
     p.parts = p.part_rows ? (N + p.part_rows - 1) / p.part_rows : 1;
+    if (p.parts > 1 && workspace_bytes < (size_t)F * (size_t)H * sizeof(float) * (size_t)p.parts) {
+        p.parts = 1;
+        p.part_rows = N;
+    }
     return p;
 }
 

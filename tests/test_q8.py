@@ -722,3 +722,24 @@ def test_python_refusals_on_device_tensors():
             call()
     torch.cuda.synchronize()
     assert bool((codes == 77).all()) and bool((scale == 0.5).all()) and bool((Y == 0).all())
+
+
+def test_workspaces_of_the_asked_size_are_taken():
+    """A size that the plan asks for is one that the plan is content with: per part F * H sums, and one part more or
+    less would show in a size between two multiples."""
+    ask = es.es_q8_weight_grad_workspace_bytes
+    for N in (1, 255, 256, 511, 513, 1025, 9_999, 40_000, 233_000, 1_000_003, 2_450_000, 2 ** 31 - 1):
+        for F, H in ((1, 1), (16, 16), (41, 7), (128, 128), (130, 65), (602, 256), (1100, 300), (5000, 4000)):
+            need = ask(N, F, H)
+            assert need % (4 * F * H) == 0
+            parts = need // (4 * F * H)
+            if parts:                                          # every part has rows: whole steps of 64, the last one some
+                rows = -(-(-(-N // parts)) // 64) * 64
+                assert 1 < parts <= 512 and rows * (parts - 1) < N <= rows * parts
+    ask = es.es_spmm_q8_workspace_bytes
+    assert ask(233_000, 10 ** 8, 64, 64, "bucket", 233_000) == 0           # no row is cut
+    assert ask(170_000, 2_400_000, 100, 0, "full", 170_000) == 4 * 100 * 2 * (2_400_000 // 1024 + 1)
+    assert ask(233_000, 114_000_000, 64, 0, "full", 32) == 4 * 64 * 32 * 64   # a few rows: 64 pieces each
+    assert ask(233_000, 300, 64, 0, "full", 32) == 4 * 64 * 32 * 3            # no row has more than 300 entries
+    for bad in ((-1, 5, 64, 4, 0, 1), (5, -1, 64, 4, 0, 1), (5, 5, 0, 4, 0, 1), (5, 5, 64, 0, 1, 1), (5, 5, 64, 4, 0, 0), (5, 5, 64, 4, 9, 1)):
+        assert ask(*bad) == 0
