@@ -119,6 +119,8 @@ int check_product(int64_t N, int64_t nnz, int32_t F, int32_t ldq, int32_t ld, in
 // Everything the host decides about one product on 8-bit rows.
 struct Q8Plan {
     int G;                     // lanes per row of codes
+    int team;                  // lanes per row of the graph
+    bool random;               // edge gradient: Q8_RANDOM
     int32_t wave_rows;         // rows a wave takes
     int64_t slices;            // blocks of 16 G columns
     bool few;                  // es_q8_few_kernel
@@ -129,6 +131,25 @@ struct Q8Plan {
 };
 
 constexpr int64_t kFewRows = 512;
+
+// Rows to waves, and which rows are long, for rows that keep `mean` entries, at most Wk.
+void plan_rows(Q8Plan& p, int64_t n_rows, double mean, int64_t Wk)
+{
+    // Rows per wave: the more, the more alike are those that run side by side; but every SIMD wants some waves.
+    const int side = kWaveSize / p.team;                       // rows side by side
+    p.wave_rows = 64;
+    while (p.wave_rows > side && p.wave_rows > 4 && n_rows / p.wave_rows < 8 * 4 * kComputeUnits) p.wave_rows /= 2;
+    // a lane retires a batch of entries in some 1.5 us; a row should not take it a tenth of the launch
+    const double us = mean * (double)n_rows * (double)(p.slices * (p.G * 16 + 12)) / 5.0e6;
+    double k = kQ8Batch * 0.07 * us;
+    if (k < 4.0 * mean) k = 4.0 * mean;
+    p.long_k = k < 64.0 ? 64 : k > 1.0e9 ? 1000000000 : (int32_t)k;
+    if (p.random) p.long_k = INT32_MAX;                        // W bounds them
+    p.long_blocks = Wk > p.long_k ? (n_rows + kQ8ScanRows - 1) / kQ8ScanRows * kQ8Share : 0;
+    p.nblocks = (n_rows + kWavesPerBlock * p.wave_rows - 1) / (kWavesPerBlock * p.wave_rows);
+    p.per_xcd = (p.nblocks + kNumXcd - 1) / kNumXcd;
+    p.grid_x = p.per_xcd * kNumXcd + p.long_blocks;
+}
 
 Q8Plan plan_q8(int64_t N, int64_t nnz, int32_t F, int32_t W, int32_t mode, int64_t n_rows, bool may_split = true)
 {
@@ -155,26 +176,30 @@ Q8Plan plan_q8(int64_t N, int64_t nnz, int32_t F, int32_t W, int32_t mode, int64
         p.piece = p.long_k = INT32_MAX;
         return p;
     }
-    // Rows per wave: the more, the more alike are those that run side by side; but every SIMD wants some waves.
-    const int side = kWaveSize / (p.G < 4 ? 4 : p.G);          // rows side by side
-    p.wave_rows = 64;
-    while (p.wave_rows > side && n_rows / p.wave_rows < 8 * 4 * kComputeUnits) p.wave_rows /= 2;
-    // a lane retires a batch of entries in some 1.5 us; a row should not take it a tenth of the launch
-    const double entries = mean * (double)n_rows;
-    const double us = entries * (double)(p.slices * (p.G * 16 + 12)) / 5.0e6;
-    double k = kQ8Batch * 0.07 * us;
-    if (k < 4.0 * mean) k = 4.0 * mean;
-    p.long_k = k < 64.0 ? 64 : k > 1.0e9 ? 1000000000 : (int32_t)k;
+    p.team = p.G < 4 ? 4 : p.G;
+    plan_rows(p, n_rows, mean, Wk);
     int64_t piece = 1024;
     while (piece * 8192 < nnz) piece *= 2;
-    p.piece = (int32_t)piece;
-    const bool long_rows = Wk > p.long_k;
     p.pieces = Wk > piece && nnz > piece ? 2 * (nnz / piece + 1) : 0;
-    if (!p.pieces) p.piece = INT32_MAX;
-    p.long_blocks = long_rows ? (n_rows + kQ8ScanRows - 1) / kQ8ScanRows * kQ8Share : 0;
-    p.nblocks = (n_rows + kWavesPerBlock * p.wave_rows - 1) / (kWavesPerBlock * p.wave_rows);
-    p.per_xcd = (p.nblocks + kNumXcd - 1) / kNumXcd;
-    p.grid_x = p.per_xcd * kNumXcd + p.long_blocks;
+    p.piece = p.pieces ? (int32_t)piece : INT32_MAX;
+    return p;
+}
+
+Q8Plan plan_vals(int64_t N, int64_t nnz, int32_t F, int32_t W, int32_t mode)
+{
+    Q8Plan p = {};
+    const int64_t chunks = ((int64_t)F + 15) / 16;
+    p.G = chunks >= 64 ? 64 : next_pow2(chunks);
+    p.slices = 1;
+    const int64_t Wk = mode == ES_FULL ? INT32_MAX : W;
+    double mean = (double)nnz / (double)N;
+    if (mean > (double)Wk) mean = (double)Wk;
+    p.team = p.G < 4 ? 4 : p.G;
+    p.random = mode == ES_FASTRAND && W <= kQ8MostRandom;
+    // FastRand: a team's kept entries wait in LDS, which holds 64 of them for each of four rows side by side, or 1024 of one
+    if (p.random) p.team = p.G <= 16 && W <= 64 ? 16 : kWaveSize;
+    plan_rows(p, N, mean < 1.0 ? 1.0 : mean, p.random ? 0 : Wk);
+    p.piece = 1024;                                            // each entry is for itself: pieces need no room and no join
     return p;
 }
 
@@ -206,6 +231,28 @@ int launch_q8(const Q8Args& a, const Q8Plan& p, hipStream_t st)
         return launched();
     }
     return ES_OK;
+}
+
+template <bool WIDE>
+int launch_vals(const Q8Args& a, const Q8Plan& p, hipStream_t st)
+{
+    const dim3 grid((uint32_t)p.grid_x), block(kBlockThreads);
+    if (a.mode == ES_FASTRAND && !p.random) {
+        hipLaunchKernelGGL(es_q8_zero_kernel, dim3(8 * kComputeUnits), block, 0, st, a);
+        if (launched() != ES_OK) return ES_ERR_LAUNCH;
+    }
+#define ES_VALS(G_, TEAM_, KIND_) hipLaunchKernelGGL((es_q8_vals_kernel<G_, TEAM_, KIND_, WIDE>), grid, block, 0, st, a)
+#define ES_Q8(G_)                                                                                              \
+    case G_:                                                                                                   \
+        if (p.random && p.team == 64) ES_VALS(G_, 64, Q8_RANDOM);                                              \
+        else if (p.random) ES_VALS(G_, (G_) <= 16 ? 16 : 64, Q8_RANDOM);                                        \
+        else if (p.long_blocks) ES_VALS(G_, (G_) < 4 ? 4 : G_, Q8_LONG);                                       \
+        else ES_VALS(G_, (G_) < 4 ? 4 : G_, Q8_PREFIX);                                                        \
+        break;
+    switch (p.G) { ES_Q8(1) ES_Q8(2) ES_Q8(4) ES_Q8(8) ES_Q8(16) ES_Q8(32) ES_Q8(64) }
+#undef ES_Q8
+#undef ES_VALS
+    return launched();
 }
 
 }  // namespace
@@ -290,15 +337,13 @@ int es_spmm_q8_backward_vals(const int32_t* rowptr, const int32_t* colidx, const
     a.rowptr = rowptr; a.colidx = colidx; a.codes = codes; a.scale = scale; a.Y = dvals; a.dY = dY;
     a.N = a.n_rows = N; a.seed = seed; a.F = F; a.ldq = ldq; a.ldy = ldy;
     a.W = mode == ES_FULL ? INT32_MAX : W; a.mode = mode; a.norm = norm;
-    uint32_t gx;
-    const int64_t chunks = ((int64_t)F + 15) / 16;
-    const int G = chunks >= 64 ? 64 : next_pow2(chunks);
-    if (!grid_of(N, kWavesPerBlock, &gx)) return ES_ERR_UNSUPPORTED;
-    hipStream_t st = static_cast<hipStream_t>(stream);
-#define ES_Q8(G_) case G_: hipLaunchKernelGGL(es_q8_vals_kernel<G_>, dim3(gx), dim3(kBlockThreads), 0, st, a); break;
-    switch (G) { ES_Q8(1) ES_Q8(2) ES_Q8(4) ES_Q8(8) ES_Q8(16) ES_Q8(32) ES_Q8(64) }
-#undef ES_Q8
-    return launched();
+    const bool wide = (uint64_t)N * (uint64_t)(ldq / kQ8Cols) > 0xFFFFFFFFull;
+    a.row_units = wide ? 0u : (uint32_t)(ldq / kQ8Cols);
+    const Q8Plan p = plan_vals(N, nnz, F, W, mode);
+    a.piece = p.piece; a.long_k = p.long_k; a.wave_rows = p.wave_rows;
+    if (p.grid_x > INT32_MAX) return ES_ERR_UNSUPPORTED;
+    a.nblocks = (uint32_t)p.nblocks; a.blocks_per_xcd = (uint32_t)p.per_xcd; a.long_blocks = (uint32_t)p.long_blocks;
+    return wide ? launch_vals<true>(a, p, static_cast<hipStream_t>(stream)) : launch_vals<false>(a, p, static_cast<hipStream_t>(stream));
 }
 
 }  // extern "C"

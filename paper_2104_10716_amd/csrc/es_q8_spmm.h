@@ -516,59 +516,251 @@ __global__ void __launch_bounds__(kBlockThreads) es_q8_few_join_kernel(const Q8A
     }
 }
 
-// One wave per row; the lanes' shares of a dot product meet in registers.  Wider rows than 16 * G columns take
-// several sweeps over the tile, whose sums meet in the tile.
-template <int G>
-__global__ void __launch_bounds__(kBlockThreads) es_q8_vals_kernel(const Q8Args a)
+// ---- the gradient of the values ---------------------------------------------------------------
+// This lane's 16 columns of a row of dY, from column c on; zeros behind the last one.
+__device__ __forceinline__ void q8_load_dy(const Q8Args& a, int64_t r, int c, float (&dy)[kQ8Cols])
 {
-    constexpr int E = kWaveSize / G;
-    __shared__ uint2 lds[kWavesPerBlock * kQ8Tile];
-    __shared__ float sums[kWavesPerBlock * kQ8Tile];
-    const int lane = threadIdx.x & (kWaveSize - 1), wave = threadIdx.x >> 6;
-    uint2* tile = lds + wave * kQ8Tile;
-    float* sum = sums + wave * kQ8Tile;
-    const int64_t i = (int64_t)blockIdx.x * kWavesPerBlock + wave;
-    const Q8Row w = q8_row(a, i);
-    if (w.n == 0) return;
-    const int e = lane / G, l = lane % G;
-    const float f = row_factor(a.norm, w.n, w.k);
-    float* out = a.Y + w.base;
-    if (w.k < w.n) {
-        const int from = a.mode == ES_BUCKET ? w.k : 0;
-        for (int p = from + lane; p < w.n; p += kWaveSize) out[p] = 0.0f;
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
-        __builtin_amdgcn_wave_barrier();
-        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");
+    typedef float float4_u __attribute__((ext_vector_type(4), aligned(4)));
+    const float* p = a.dY + r * (int64_t)a.ldy + c;
+#pragma unroll
+    for (int j = 0; j < kQ8Cols; j += 4) {
+        float4_u v = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (c + j + 4 <= a.F) {
+            v = *reinterpret_cast<const float4_u*>(p + j);
+        } else {
+#pragma unroll
+            for (int m = 0; m < 4; ++m)
+                if (c + j + m < a.F) v[m] = p[j + m];
+        }
+#pragma unroll
+        for (int m = 0; m < 4; ++m) dy[j + m] = v[m];
     }
-    RowSampler s;
-    s.init(a.mode, a.seed, w.r, (uint32_t)w.n, (uint32_t)a.W, (uint32_t)lane, kWaveSize);
-    for (int t0 = 0; t0 < w.k; t0 += kQ8Tile) {
-        const int count = min(w.k - t0, kQ8Tile);
-        sample_tile(s, lane, kWaveSize, count, [&](int slot, uint32_t entry) {
-            tile[slot] = make_uint2((uint32_t)a.colidx[(int64_t)w.base + entry], entry);
-        });
-        wave_lds_fence();
-        for (int c = l * kQ8Cols; c - l * kQ8Cols < a.F; c += G * kQ8Cols) {
-            float dy[kQ8Cols];
+}
+
+// One tile of a row: TEAM lanes stage up to 4 TEAM entries, lane t those of slots t, t + TEAM, ...; edge slot e then takes the
+// entries of the lanes e G .. e G + G - 1, one after the other: G lanes multiply, their shares meet in registers, and the lane that
+// staged an entry keeps its product.  `most`, `spare` as in q8_tile.  The gradients
+// go to the entries' places, or by slot into `result` (LDS).  Rows wider than 16 G columns (G = 64) take several sweeps.
+template <int G, int TEAM, bool WIDE>
+__device__ __forceinline__ void q8_dots(const Q8Args& a, RowSampler& s, int t, int count, int most, int32_t base, int32_t spare,
+                                        int64_t r, uint32_t* tile, float (&dy)[kQ8Cols], float f, float* result)
+{
+    constexpr int U = G < 4 ? G : 4;
+    const int l = t & (G - 1), e = t / G;
+    int64_t p[4];
+    int32_t c[4];
+    float w[4], d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-            for (int j = 0; j < kQ8Cols; ++j) dy[j] = c + j < a.F ? a.dY[w.r * (int64_t)a.ldy + c + j] : 0.0f;
-            const int8_t* codes = a.codes + (c < a.F ? c : 0);
-            for (int j0 = 0; j0 < count; j0 += E) {
-                const int j = j0 + e;
-                float d = 0.0f;
-                if (j < count) {
-                    const uint4_v q = *reinterpret_cast<const uint4_v*>(codes + (int64_t)tile[j].x * a.ldq);
+    for (int m = 0; m < 4; ++m) {
+        const uint32_t entry = s.next();
+        p[m] = t + m * TEAM < count ? (int64_t)base + entry : (int64_t)spare;
+        c[m] = a.colidx[p[m]];
+    }
 #pragma unroll
-                    for (int m = 0; m < kQ8Cols; ++m) d = fmaf(dy[m], (float)(int8_t)(q[m / 4] >> (8 * (m % 4))), d);
+    for (int m = 0; m < 4; ++m) {
+        w[m] = a.scale[c[m]] * f;
+        tile[t + m * TEAM] = q8_key<WIDE>(a, c[m]);
+    }
+    wave_lds_fence();
+    const uint32_t* key = tile + e * G;
+    for (int c0 = l * kQ8Cols; c0 - l * kQ8Cols < a.F; c0 += G * kQ8Cols) {
+        if constexpr (G == 64) q8_load_dy(a, r < 0 ? 0 : r, c0, dy);
+        const int8_t* codes = a.codes + (c0 < a.F ? c0 : 0);
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+            if (m * TEAM >= most) break;                       // wave-uniform
+#pragma unroll 1
+            for (int u0 = 0; u0 < G; u0 += U) {
+                if (TEAM == G && m * TEAM + u0 >= most) break;
+                uint4_v q[U];
+#pragma unroll
+                for (int u = 0; u < U; ++u) q[u] = q8_load<WIDE>(a, codes, key[m * TEAM + u0 + u]);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    float x = 0.0f;
+#pragma unroll
+                    for (int j = 0; j < kQ8Cols; ++j) x = fmaf(dy[j], (float)(int8_t)(q[u][j / 4] >> (8 * (j % 4))), x);
+                    x = team_reduce<G>(x, [](float y, float z) { return y + z; });
+                    d[m] += l == u0 + u ? x : 0.0f;
+                    __builtin_amdgcn_sched_barrier(0);
                 }
-                d = team_reduce<G>(d, [](float x, float y) { return x + y; });
-                if (l == 0 && j < count) sum[j] = c == l * kQ8Cols ? d : sum[j] + d;
             }
         }
+    }
+#pragma unroll
+    for (int m = 0; m < 4; ++m) {
+        if (t + m * TEAM >= count) continue;
+        if (result) result[t + m * TEAM] = d[m] * w[m];
+        else a.Y[p[m]] = d[m] * w[m];
+    }
+    wave_lds_fence();
+}
+
+// dvals of entries [from, to), zeros; by `lanes` lanes
+__device__ __forceinline__ void q8_zero(float* out, int64_t from, int64_t to, int lane, int lanes)
+{
+    typedef float float4_u __attribute__((ext_vector_type(4), aligned(4)));
+    const float4_u zero = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int64_t p = from + 4 * lane; p < to; p += 4 * lanes) {
+        if (p + 4 <= to) {
+            *reinterpret_cast<float4_u*>(out + p) = zero;
+        } else {
+            for (int64_t q = p; q < to; ++q) out[q] = 0.0f;
+        }
+    }
+}
+
+// FastRand with W beyond what a wave can order in LDS: all gradients are cleared before any is written.
+__global__ void __launch_bounds__(kBlockThreads) es_q8_zero_kernel(const Q8Args a)
+{
+    const int64_t from = a.rowptr[0], to = a.rowptr[a.N];
+    q8_zero(a.Y, from, to, (int)(blockIdx.x * kBlockThreads + threadIdx.x), (int)(gridDim.x * kBlockThreads));
+}
+
+// Which slot of a FastRand row reads its entry 0, 1, ...: slot (idx - off) P^-1 mod n, Equation 2 solved for the slot.
+struct Q8Slots {
+    double inv_n;
+    uint32_t slot0, step;                                      // entry 0's slot, and from one entry to the next
+};
+
+// (a * b) mod n for b < n < 2^31, a < 2^31, with 1 / n at hand
+__device__ __forceinline__ uint32_t q8_mulmod(uint32_t a, uint32_t b, uint32_t n, double inv_n)
+{
+    const uint64_t q = (uint64_t)((double)a * (double)b * inv_n);          // off by one at most
+    int64_t rem = (int64_t)((uint64_t)a * b - q * n);
+    if (rem < 0) rem += n;
+    if (rem >= (int64_t)n) rem -= n;
+    return (uint32_t)rem;
+}
+
+__device__ __forceinline__ Q8Slots q8_slots(const Q8Kept& w)
+{
+    Q8Slots s = {1.0 / (double)max(w.n, 1), 0u, 1u};           // a row kept whole: entry idx is slot idx
+    if (w.mult) {
+        // With n = P a + r: P x = 1 + n m for m = -r^-1 mod P, so x = P^-1 mod n = a m + (1 + r m) / P.  P is a prime below
+        // 600 that does not divide n.
+        const uint32_t P = w.mult, n = (uint32_t)w.n, a = n / P, r = n % P;
+        int32_t u = (int32_t)P, v = (int32_t)r, x0 = 0, x1 = 1;            // u = x0 r, v = x1 r (mod P)
+        while (v > 1) {
+            const int32_t q = u / v, next = u - q * v, x = x0 - q * x1;
+            u = v; v = next; x0 = x1; x1 = x;
+        }
+        const uint32_t m = x1 < 0 ? (uint32_t)-x1 : P - (uint32_t)x1;
+        s.step = a * m + (1u + r * m) / P;
+        s.slot0 = w.first ? q8_mulmod(n - w.first, s.step, n, s.inv_n) : 0u;
+    }
+    return s;
+}
+
+constexpr int32_t kQ8MostRandom = 1024;                        // largest W whose gradients a wave orders in LDS
+
+enum { Q8_PREFIX = 0, Q8_LONG = 1, Q8_RANDOM = 2 };
+
+// Rows and waves as in es_q8_spmm_kernel.  What is not kept gets its zeros in the same pass:
+//  * Q8_PREFIX: all of a row is kept, or its first entries (full, Bucket); the wave clears what is behind them
+//  * Q8_LONG: the same where there may be long rows; here and in Q8_PREFIX FastRand's zeros are there before (es_q8_zero_kernel)
+//  * Q8_RANDOM: the kept entries lie anywhere in the row.  Zeros and gradients written one after the other would be two
+//    writes of each line, the second of single numbers; instead the gradients stay in LDS by slot, and each
+//    entry looks up whether a slot reads it, so that the row is written once, in order.
+template <int G, int TEAM, int KIND, bool WIDE>
+__global__ void __launch_bounds__(kBlockThreads, 4) es_q8_vals_kernel(const Q8Args a)
+{
+    constexpr int ROWS = kWaveSize / TEAM, T = 4 * TEAM;
+    constexpr int RESULTS = KIND != Q8_RANDOM ? 1 : TEAM == kWaveSize ? kQ8MostRandom : 4 * TEAM;   // kept entries of a row
+    __shared__ uint32_t lds[kWavesPerBlock * kQ8Tile];
+    __shared__ float results[kWavesPerBlock * ROWS * RESULTS];
+    __shared__ Q8Slots slots[KIND == Q8_RANDOM ? kWavesPerBlock * kWaveSize : 1];
+    __shared__ union { Q8Kept kept[kWavesPerBlock][kWaveSize]; Q8Scan scan; } sh;
+    const int lane = threadIdx.x & (kWaveSize - 1), wave = threadIdx.x >> 6;
+    float dy[kQ8Cols];
+    if constexpr (KIND == Q8_LONG) {
+        if (blockIdx.x < a.long_blocks) {
+            const int64_t first = (int64_t)(blockIdx.x / kQ8Share) * kQ8ScanRows;
+            const int total = q8_scan(a, first, sh.scan);
+            for (int task = (blockIdx.x + blockIdx.x / kQ8Share) % kQ8Share; task < total; task += kQ8Share) {
+                int piece, t0, count;
+                const Q8Row w = q8_row(a, first + q8_find(sh.scan, task, piece));
+                q8_piece_slots(a, w, piece, t0, count);
+                if (a.mode == ES_BUCKET && t0 == 0) q8_zero(a.Y, (int64_t)w.base + w.k, (int64_t)w.base + w.n, threadIdx.x, kBlockThreads);
+                if constexpr (G < 64) q8_load_dy(a, w.r, (lane & (G - 1)) * kQ8Cols, dy);
+                const float f = row_factor(a.norm, w.n, w.k);
+                for (int s0 = wave * kWaveSize; s0 < count; s0 += kBlockThreads) {
+                    RowSampler s;
+                    s.init(a.mode, a.seed, w.r, (uint32_t)w.n, (uint32_t)a.W, (uint32_t)(t0 + s0 + lane), kWaveSize);
+                    const int m = min(count - s0, kWaveSize);
+                    q8_dots<G, kWaveSize, WIDE>(a, s, lane, m, m, w.base, w.base, w.r, lds + wave * kQ8Tile, dy, f, nullptr);
+                }
+            }
+            return;
+        }
+    }
+    const uint32_t b = blockIdx.x - a.long_blocks;
+    const uint32_t vb = (b % kNumXcd) * a.blocks_per_xcd + b / kNumXcd;
+    if (vb >= a.nblocks) return;
+    const int64_t first_row = ((int64_t)vb * kWavesPerBlock + wave) * a.wave_rows;
+    Q8Kept* kept = sh.kept[wave];
+    Q8Slots* slot = slots + (KIND == Q8_RANDOM ? wave * kWaveSize : 0);
+    q8_plan_rows(a, first_row, lane, kept);
+    if constexpr (KIND == Q8_RANDOM) {
+        slot[lane] = q8_slots(kept[lane]);
         wave_lds_fence();
-        for (int j = lane; j < count; j += kWaveSize)
-            out[tile[j].y] = sum[j] * (a.scale[tile[j].x] * f);
-        wave_lds_fence();
+    }
+    const int rs = lane / TEAM, t = lane & (TEAM - 1);
+    uint32_t* tile = lds + wave * kQ8Tile + rs * T;
+    float* result = results + wave * ROWS * RESULTS;
+    for (int p0 = 0; p0 < a.wave_rows; p0 += ROWS) {
+        const Q8Kept w = kept[p0 + rs];
+        const int64_t r = w.place < 0 ? -1 : first_row + w.place;
+        const int most = __builtin_amdgcn_readfirstlane(w.k), spare = __builtin_amdgcn_readfirstlane(w.base);
+        if (most == 0) break;                                  // and so are all that follow
+        RowSampler s;
+        q8_sampler(s, w, t, TEAM);
+        if constexpr (G < 64) q8_load_dy(a, r < 0 ? 0 : r, (t & (G - 1)) * kQ8Cols, dy);
+        const float f = row_factor(a.norm, w.n, w.k);
+        for (int t0 = 0; t0 < most; t0 += T)
+            q8_dots<G, TEAM, WIDE>(a, s, t, w.k - t0, min(most - t0, T), w.base, spare, r, tile, dy, f,
+                                   KIND == Q8_RANDOM ? result + rs * RESULTS + t0 : nullptr);
+        if constexpr (KIND == Q8_RANDOM) {
+            // the whole wave on one row after the other, four entries of it per lane
+            for (int x = 0; x < ROWS; ++x) {
+                const Q8Kept o = kept[p0 + x];
+                const Q8Slots z = slot[p0 + x];
+                const uint32_t n = (uint32_t)__builtin_amdgcn_readfirstlane(o.n), k = (uint32_t)__builtin_amdgcn_readfirstlane(o.k);
+                if (k == 0) break;
+                typedef float float4_u __attribute__((ext_vector_type(4), aligned(4)));
+                const uint32_t jump = q8_mulmod(4 * kWaveSize, z.step, n, z.inv_n);
+                uint32_t at = z.slot0 + q8_mulmod(4u * lane, z.step, n, z.inv_n);
+                if (at >= n) at -= n;
+                float* out = a.Y + o.base;
+                for (uint32_t idx = 4u * lane; idx < n; idx += 4 * kWaveSize) {
+                    float4_u v;
+                    uint32_t i = at;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        v[j] = i < k ? result[x * RESULTS + i] : 0.0f;
+                        i += z.step;
+                        if (i >= n) i -= n;
+                    }
+                    if (idx + 4 <= n) {
+                        *reinterpret_cast<float4_u*>(out + idx) = v;
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            if (idx + j < n) out[idx + j] = v[j];
+                    }
+                    at += jump;
+                    if (at >= n) at -= n;
+                }
+            }
+            wave_lds_fence();
+        }
+    }
+    if (KIND != Q8_RANDOM && a.mode == ES_BUCKET) {
+        for (int x = 0; x < a.wave_rows; ++x) {
+            const Q8Kept o = kept[x];
+            if (o.place >= 0) q8_zero(a.Y, (int64_t)o.base + o.k, (int64_t)o.base + o.n, lane, kWaveSize);
+        }
     }
 }
 
