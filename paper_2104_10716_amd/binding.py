@@ -164,6 +164,10 @@ def load_marshal():
     _es_marshal.bind(*(ctypes.cast(f, ctypes.c_void_p).value
                        for f in (lib.es_spmm_ws, lib.es_spmm_backward, lib.es_spmm_backward_pull,
                                  lib.es_spmm_backward_ws, lib.es_spmm_backward_workspace_bytes)))
+    _es_marshal.bind_q8(*(ctypes.cast(f, ctypes.c_void_p).value
+                          for f in (lib.es_q8_write, lib.es_q8_read, lib.es_spmm_q8, lib.es_spmm_q8_workspace_bytes,
+                                    lib.es_spmm_q8_backward_vals, lib.es_q8_weight_grad,
+                                    lib.es_q8_weight_grad_workspace_bytes)))
     _marshal = _es_marshal
     return _marshal
 
@@ -648,20 +652,28 @@ def _checked(rc, where):
         raise EsSpmmError(rc, where)
 
 
+def _done(rc, where) -> bool:
+    """Whether the native marshalling took the call (None: it did not)."""
+    if rc is None:
+        return False
+    _checked(rc, where)
+    return True
+
+
 def _workspace(workspace, need, stream):
     """(workspace, bytes): the caller's, or `need` bytes from torch's allocator in the pool of the stream that will use
-    them: given back when the call returns, they are handed out again in that stream's order only."""
+    them: given back when the call returns, they are handed out again in that stream's order only.  A captured
+    stream is lent none: its graph would outlive them."""
     import torch
     if workspace is None:
         if not need:
             return None, 0
         if isinstance(stream, int):
             stream = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
-        if stream is None:
+        with torch.cuda.stream(stream or torch.cuda.current_stream()):
+            if torch.cuda.is_current_stream_capturing():
+                return None, 0
             workspace = torch.empty(need, dtype=torch.uint8, device="cuda")
-        else:
-            with torch.cuda.stream(stream):
-                workspace = torch.empty(need, dtype=torch.uint8, device="cuda")
     elif not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous device tensor")
     return workspace, workspace.numel() * workspace.element_size()
@@ -677,6 +689,8 @@ def es_q8_write(X, codes, scale, rows=None, stream=None):
     """Writes the rows of X [n, F] (float32, float16 or bfloat16) into the table (codes [N, es_q8_row_bytes(F)]
     int8, scale [N] float32): row i becomes row rows[i] (int32; ids outside [0, N) are skipped, of
     equal ids the last row is written), or without `rows` row i.  Returns (codes, scale)."""
+    if _done((_marshal or load_marshal()).q8_write(X, codes, scale, rows, stream), "es_q8_write"):
+        return codes, scale
     st = _here(stream, X=X, codes=codes, scale=scale, rows=rows)
     n, F, ldx = _matrix(X, "X")
     if F < 1:
@@ -692,6 +706,8 @@ def es_q8_write(X, codes, scale, rows=None, stream=None):
 def es_q8_read(codes, scale, Y, rows=None, stream=None):
     """Reads rows of the table into Y [n, F] (float32, float16 or bfloat16): row rows[i] (int32; ids outside
     [0, N) give zeros), or without `rows` row i.  Returns Y."""
+    if _done((_marshal or load_marshal()).q8_read(codes, scale, Y, rows, stream), "es_q8_read"):
+        return Y
     st = _here(stream, codes=codes, scale=scale, Y=Y, rows=rows)
     n, F, ldy = _matrix(Y, "Y")
     if F < 1:
@@ -723,8 +739,10 @@ def es_spmm_q8(rowptr, colidx, vals, codes, scale, Y, W: int, mode, seed: int = 
                stream=None):
     """Y[i] = f * sum of vals[p] * (row colidx[p] of the table) over the kept entries p of row rows[i] (int32 ids
     in any order; outside [0, N): zeros), or of every row; Y float32 [n, F].  `workspace`: a contiguous device
-    tensor of es_spmm_q8_workspace_bytes(N, len(colidx), F, W, mode, n) bytes; by default one from torch's allocator.
-    Returns Y."""
+    tensor of es_spmm_q8_workspace_bytes(N, len(colidx), F, W, mode, n) bytes; by default one from torch's allocator, and on
+    a captured stream none: very long rows, and few asked ones, are then slower.  Returns Y."""
+    if _done((_marshal or load_marshal()).spmm_q8(rowptr, colidx, vals, codes, scale, Y, W, mode, seed, norm, rows, workspace, stream), "es_spmm_q8"):
+        return Y
     import torch
     st = _here(stream, rowptr=rowptr, colidx=colidx, vals=vals, codes=codes, scale=scale, Y=Y, rows=rows, workspace=workspace)
     n, F, ldy = _matrix(Y, "Y")
@@ -749,6 +767,8 @@ def es_spmm_q8(rowptr, colidx, vals, codes, scale, Y, W: int, mode, seed: int = 
 def es_spmm_q8_backward_vals(rowptr, colidx, dY, codes, scale, dvals, W: int, mode, seed: int = 0, norm="none", stream=None):
     """dvals[p] = f * (dY[r] . row c of the table) for the kept entries p = (r, c), 0 for the others: the gradient of
     es_spmm_q8's and es_spmm_norm's Y with respect to `vals`; dY float32 [N, F], dvals float32 [nnz].  Returns dvals."""
+    if _done((_marshal or load_marshal()).q8_vals(rowptr, colidx, dY, codes, scale, dvals, W, mode, seed, norm, stream), "es_spmm_q8_backward_vals"):
+        return dvals
     import torch
     st = _here(stream, rowptr=rowptr, colidx=colidx, dY=dY, codes=codes, scale=scale, dvals=dvals)
     n, F, ldy = _matrix(dY, "dY")
@@ -772,7 +792,10 @@ def es_q8_weight_grad_workspace_bytes(N: int, F: int, H: int) -> int:
 
 def es_q8_weight_grad(codes, scale, G, dW, workspace=None, stream=None):
     """dW [F, H] = (the table's N rows of F values)^T @ G [N, H], float32.  `workspace`: a contiguous device tensor of
-    es_q8_weight_grad_workspace_bytes(N, F, H) bytes; by default one from torch's allocator.  Returns dW."""
+    es_q8_weight_grad_workspace_bytes(N, F, H) bytes; by default one from torch's allocator, and on a captured stream none:
+    pass one there, or many rows are summed by few workgroups.  Returns dW."""
+    if _done((_marshal or load_marshal()).q8_weight_grad(codes, scale, G, dW, workspace, stream), "es_q8_weight_grad"):
+        return dW
     import torch
     st = _here(stream, codes=codes, scale=scale, G=G, dW=dW, workspace=workspace)
     n, H, ldg = _matrix(G, "G")

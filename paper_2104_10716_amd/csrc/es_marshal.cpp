@@ -26,6 +26,13 @@ decltype(&es_spmm_backward) g_backward = nullptr;
 decltype(&es_spmm_backward_ws) g_backward_ws = nullptr;
 decltype(&es_spmm_backward_workspace_bytes) g_backward_bytes = nullptr;
 decltype(&es_spmm_backward_pull) g_pull = nullptr;
+decltype(&es_q8_write) g_q8_write = nullptr;
+decltype(&es_q8_read) g_q8_read = nullptr;
+decltype(&es_spmm_q8) g_spmm_q8 = nullptr;
+decltype(&es_spmm_q8_workspace_bytes) g_spmm_q8_bytes = nullptr;
+decltype(&es_spmm_q8_backward_vals) g_q8_vals = nullptr;
+decltype(&es_q8_weight_grad) g_q8_grad = nullptr;
+decltype(&es_q8_weight_grad_workspace_bytes) g_q8_grad_bytes = nullptr;
 
 // Strided, with a storage that holds its elements, and not a Python-dispatched
 // wrapper.  A fake tensor calls itself a device tensor and answers with a null
@@ -312,6 +319,213 @@ PyObject* pull(PyObject*, PyObject* const* a, Py_ssize_t n)
     });
 }
 
+// ---- 8-bit rows: tensors have to be on the current device -------------------------------------
+bool here(PyObject* o, at::ScalarType type, const at::Tensor** out)
+{
+    return as_tensor(o, type, out) && (*out)->get_device() == c10::hip::current_device();
+}
+
+// A dense matrix with unit column stride and at least one column.
+struct Matrix {
+    void* p;
+    int64_t n;
+    int32_t F, ld;
+
+    bool parse(const at::Tensor& t)
+    {
+        if (t.dim() != 2 || t.size(1) < 1 || t.size(1) > INT32_MAX || (t.size(1) > 1 && t.stride(1) != 1)) return false;
+        const int64_t s = t.size(0) > 1 ? t.stride(0) : t.size(1);
+        if (s < t.size(1) || s > INT32_MAX) return false;
+        p = t.data_ptr(); n = t.size(0); F = (int32_t)t.size(1); ld = (int32_t)s;
+        return true;
+    }
+    bool parse(PyObject* o, at::ScalarType type)
+    {
+        const at::Tensor* t;
+        return here(o, type, &t) && parse(*t);
+    }
+    // of one of the types that a table is written from and read to
+    bool parse_any(PyObject* o, int32_t* type)
+    {
+        const at::ScalarType types[] = {at::kFloat, at::kHalf, at::kBFloat16};     // in the order of es_type_t
+        for (int i = 0; i < 3; ++i)
+            if (parse(o, types[i])) { *type = i; return true; }
+        return false;
+    }
+};
+
+struct Table {
+    const int8_t* codes;
+    const float* scale;
+    int64_t N;
+    int32_t ldq;
+
+    bool parse(PyObject* c, PyObject* s, int32_t F)
+    {
+        Matrix m;
+        const at::Tensor* t;
+        if (!m.parse(c, at::kChar) || !here(s, at::kFloat, &t) || t->dim() != 1 || t->size(0) != m.n || !t->is_contiguous()) return false;
+        if (m.F < ((int64_t)F + 15) / 16 * 16 || m.ld % 16 || reinterpret_cast<uintptr_t>(m.p) % 16) return false;
+        codes = static_cast<const int8_t*>(m.p); N = m.n; ldq = m.ld;
+        scale = static_cast<const float*>(t->data_ptr());
+        return true;
+    }
+};
+
+// A contiguous vector of `n` elements, or (optional) None.
+bool vector(PyObject* o, at::ScalarType type, int64_t n, bool optional, void** out)
+{
+    *out = nullptr;
+    if (optional && o == Py_None) return true;
+    const at::Tensor* t;
+    if (!here(o, type, &t) || t->dim() != 1 || t->size(0) != n || !t->is_contiguous()) return false;
+    *out = t->data_ptr();
+    return true;
+}
+
+// The caller's workspace, or None.
+bool workspace_of(PyObject* o, void** p, size_t* bytes)
+{
+    *p = nullptr;
+    *bytes = 0;
+    if (o == Py_None) return true;
+    if (!THPVariable_Check(o)) return false;
+    const at::Tensor& t = THPVariable_Unpack(o);
+    if (!t.is_cuda() || !has_memory(t) || !t.is_contiguous() || t.get_device() != c10::hip::current_device()) return false;
+    *p = t.nbytes() ? t.data_ptr() : nullptr;
+    *bytes = t.nbytes();
+    return true;
+}
+
+// bind_q8(es_q8_write, es_q8_read, es_spmm_q8, es_spmm_q8_workspace_bytes, es_spmm_q8_backward_vals, es_q8_weight_grad,
+// es_q8_weight_grad_workspace_bytes): addresses of the C entry points
+PyObject* bind_q8(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    void* p[7] = {};
+    for (int i = 0; i < 7 && n == 7; ++i) p[i] = PyLong_AsVoidPtr(a[i]);
+    for (void* q : p)
+        if (!q) {
+            if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "bind_q8 takes seven addresses");
+            return nullptr;
+        }
+    g_q8_write = reinterpret_cast<decltype(g_q8_write)>(p[0]);
+    g_q8_read = reinterpret_cast<decltype(g_q8_read)>(p[1]);
+    g_spmm_q8 = reinterpret_cast<decltype(g_spmm_q8)>(p[2]);
+    g_spmm_q8_bytes = reinterpret_cast<decltype(g_spmm_q8_bytes)>(p[3]);
+    g_q8_vals = reinterpret_cast<decltype(g_q8_vals)>(p[4]);
+    g_q8_grad = reinterpret_cast<decltype(g_q8_grad)>(p[5]);
+    g_q8_grad_bytes = reinterpret_cast<decltype(g_q8_grad_bytes)>(p[6]);
+    Py_RETURN_NONE;
+}
+
+// q8_write(X, codes, scale, rows, stream)
+PyObject* q8_write(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    Matrix x;
+    Table t;
+    int32_t type;
+    void *rows, *stream;
+    if (n != 5 || !g_q8_write || !as_stream(a[4], &stream) || !x.parse_any(a[0], &type) || !t.parse(a[1], a[2], x.F) ||
+        !vector(a[3], at::kInt, x.n, true, &rows) || (a[3] == Py_None && x.n > t.N))
+        Py_RETURN_NONE;
+    return unlocked([&] {
+        return g_q8_write(x.p, type, x.n, x.F, x.ld, static_cast<const int32_t*>(rows), t.N, const_cast<int8_t*>(t.codes), t.ldq,
+                          const_cast<float*>(t.scale), stream);
+    });
+}
+
+// q8_read(codes, scale, Y, rows, stream)
+PyObject* q8_read(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    Matrix y;
+    Table t;
+    int32_t type;
+    void *rows, *stream;
+    if (n != 5 || !g_q8_read || !as_stream(a[4], &stream) || !y.parse_any(a[2], &type) || !t.parse(a[0], a[1], y.F) ||
+        !vector(a[3], at::kInt, y.n, true, &rows) || (a[3] == Py_None && y.n > t.N))
+        Py_RETURN_NONE;
+    return unlocked([&] {
+        return g_q8_read(t.codes, t.ldq, t.scale, t.N, y.F, static_cast<const int32_t*>(rows), y.n, y.p, type, y.ld, stream);
+    });
+}
+
+// The graph beside a table of N rows.
+struct Q8Graph {
+    const int32_t *rowptr, *colidx;
+    int64_t nnz;
+
+    bool parse(PyObject* rp, PyObject* ci, int64_t N)
+    {
+        const at::Tensor* c;
+        void* r;
+        if (!vector(rp, at::kInt, N + 1, false, &r) || !here(ci, at::kInt, &c) || c->dim() != 1 || !c->is_contiguous()) return false;
+        rowptr = static_cast<const int32_t*>(r);
+        colidx = static_cast<const int32_t*>(c->data_ptr());
+        nnz = c->size(0);
+        return true;
+    }
+};
+
+// spmm_q8(rowptr, colidx, vals, codes, scale, Y, W, mode, seed, norm, rows, workspace, stream)
+PyObject* spmm_q8(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    Product s;
+    Matrix y;
+    Table t;
+    Q8Graph g;
+    void *vals, *rows, *ws;
+    size_t bytes;
+    if (n != 13 || !g_spmm_q8 || !s.scalars(a[6], a[7], a[8], a[9], Py_None, a[12]) || !y.parse(a[5], at::kFloat) ||
+        !t.parse(a[3], a[4], y.F) || !g.parse(a[0], a[1], t.N) || !vector(a[2], at::kFloat, g.nnz, true, &vals) ||
+        !vector(a[10], at::kInt, y.n, true, &rows) || (a[10] == Py_None && y.n != t.N) || !workspace_of(a[11], &ws, &bytes))
+        Py_RETURN_NONE;
+    return unlocked([&] {
+        const size_t need = a[11] == Py_None ? g_spmm_q8_bytes(t.N, g.nnz, y.F, s.W, s.mode, y.n) : 0;
+        const Scratch lent(need, static_cast<hipStream_t>(s.stream));
+        if (lent.p) { ws = lent.p; bytes = need; }
+        return g_spmm_q8(g.rowptr, g.colidx, static_cast<const float*>(vals), t.codes, t.ldq, t.scale, static_cast<float*>(y.p), t.N,
+                         g.nnz, y.F, y.ld, s.W, s.mode, s.seed, s.norm, static_cast<const int32_t*>(rows), y.n, ws, bytes, s.stream);
+    });
+}
+
+// q8_vals(rowptr, colidx, dY, codes, scale, dvals, W, mode, seed, norm, stream)
+PyObject* q8_vals(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    Product s;
+    Matrix dy;
+    Table t;
+    Q8Graph g;
+    void* dvals;
+    if (n != 11 || !g_q8_vals || !s.scalars(a[6], a[7], a[8], a[9], Py_None, a[10]) || !dy.parse(a[2], at::kFloat) ||
+        !t.parse(a[3], a[4], dy.F) || dy.n != t.N || !g.parse(a[0], a[1], t.N) || !vector(a[5], at::kFloat, g.nnz, false, &dvals))
+        Py_RETURN_NONE;
+    return unlocked([&] {
+        return g_q8_vals(g.rowptr, g.colidx, static_cast<const float*>(dy.p), dy.ld, t.codes, t.ldq, t.scale, static_cast<float*>(dvals),
+                         t.N, g.nnz, dy.F, s.W, s.mode, s.seed, s.norm, s.stream);
+    });
+}
+
+// q8_weight_grad(codes, scale, G, dW, workspace, stream)
+PyObject* q8_weight_grad(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    Matrix g, w;
+    Table t;
+    const at::Tensor* dw;
+    void *ws, *stream;
+    size_t bytes;
+    if (n != 6 || !g_q8_grad || !as_stream(a[5], &stream) || !g.parse(a[2], at::kFloat) || !here(a[3], at::kFloat, &dw) ||
+        !w.parse(*dw) || w.n < 1 || w.n > INT32_MAX || w.F != g.F || !t.parse(a[0], a[1], (int32_t)w.n) || g.n != t.N ||
+        !workspace_of(a[4], &ws, &bytes))
+        Py_RETURN_NONE;
+    return unlocked([&] {
+        const size_t need = a[4] == Py_None ? g_q8_grad_bytes(t.N, (int32_t)w.n, g.F) : 0;
+        const Scratch lent(need, static_cast<hipStream_t>(stream));
+        if (lent.p) { ws = lent.p; bytes = need; }
+        return g_q8_grad(t.codes, t.ldq, t.scale, static_cast<const float*>(g.p), g.ld, static_cast<float*>(w.p), w.ld, t.N, (int32_t)w.n,
+                         g.F, ws, bytes, stream);
+    });
+}
+
 // readable(tensor): whether has_memory holds
 PyObject* readable(PyObject*, PyObject* const* a, Py_ssize_t n)
 {
@@ -333,6 +547,8 @@ PyObject* guarded(PyObject* self, PyObject* const* a, Py_ssize_t n)
 
 #define ES_METHOD(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(guarded<f>)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {ES_METHOD(bind), ES_METHOD(spmm), ES_METHOD(backward), ES_METHOD(pull), ES_METHOD(readable),
+                         ES_METHOD(bind_q8), ES_METHOD(q8_write), ES_METHOD(q8_read), ES_METHOD(spmm_q8), ES_METHOD(q8_vals),
+                         ES_METHOD(q8_weight_grad),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_es_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

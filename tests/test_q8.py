@@ -744,3 +744,52 @@ def test_workspaces_of_the_asked_size_are_taken():
     assert ask(233_000, 300, 64, 0, "full", 32) == 4 * 64 * 32 * 3            # no row has more than 300 entries
     for bad in ((-1, 5, 64, 4, 0, 1), (5, -1, 64, 4, 0, 1), (5, 5, 0, 4, 0, 1), (5, 5, 64, 0, 1, 1), (5, 5, 64, 4, 0, 0), (5, 5, 64, 4, 9, 1)):
         assert ask(*bad) == 0
+
+
+@pytest.mark.gpu
+def test_native_marshalling_agrees_with_the_checks_in_python(monkeypatch):
+    """The plain calls go through the native marshalling; what it hands back goes through the checks in Python to
+    the same kernels.  Streams and integers of every kind."""
+    import torch
+    m = es.load_marshal()
+    N, F, H = 600, 40, 24
+    rowptr, colidx = graph(N, 10.0, 3, long_row=590)
+    rng = np.random.default_rng(3)
+    rp, ci, a = dev(rowptr), dev(colidx), dev(rng.standard_normal(colidx.size).astype(np.float32))
+    X = dev(rng.standard_normal((N, F)).astype(np.float32))
+    G = dev(rng.standard_normal((N, H)).astype(np.float32))
+    ids = dev(rng.integers(-1, N, 50).astype(np.int32))
+    side = torch.cuda.Stream()
+
+    def everything(stream, W, seed):
+        new = lambda *s: torch.zeros(s, device="cuda:0")  # noqa: E731
+        codes, scale = table(N, F)
+        torch.cuda.synchronize()
+        es.es_q8_write(X, codes, scale, stream=stream)
+        es.es_q8_write(X[:50], codes, scale, rows=ids, stream=stream)
+        out = [codes, scale, es.es_q8_read(codes, scale, new(50, F), rows=ids, stream=stream),
+               es.es_q8_read(codes, scale, new(N, F).bfloat16(), stream=stream),
+               es.es_spmm_q8(rp, ci, a, codes, scale, new(N, F), W, "full", seed, "mean", stream=stream),
+               es.es_spmm_q8(rp, ci, None, codes, scale, new(50, F), W, "fastrand", seed, "none", rows=ids, stream=stream),
+               es.es_spmm_q8_backward_vals(rp, ci, X, codes, scale, new(colidx.size), W, "fastrand", seed, stream=stream),
+               es.es_q8_weight_grad(codes, scale, G, new(F, H), stream=stream)]
+        torch.cuda.synchronize()
+        return out
+
+    want = everything(None, 7, 5)
+    taken = m.q8_write(X, want[0].clone(), want[1].clone(), None, None)
+    assert taken == 0                                          # the native path, not a fallback
+    for stream, W, seed in ((side, np.int64(7), np.uint64(5)), (side.cuda_stream, 7, 2 ** 64 + 5), (0, True * 7, 5)):
+        for got, w in zip(everything(stream, W, seed), want):
+            assert torch.equal(got, w)
+
+    class Refusing:
+        readable = staticmethod(m.readable)
+
+        def __getattr__(self, name):
+            return lambda *a: None
+
+    monkeypatch.setattr(es.binding, "_marshal", Refusing())
+    for stream in (None, side, side.cuda_stream):
+        for got, w in zip(everything(stream, 7, 5), want):
+            assert torch.equal(got, w)
