@@ -604,7 +604,7 @@ __device__ __forceinline__ void q8_zero(float* out, int64_t from, int64_t to, in
     const float4_u zero = {0.0f, 0.0f, 0.0f, 0.0f};
     for (int64_t p = from + 4 * lane; p < to; p += 4 * lanes) {
         if (p + 4 <= to) {
-            *reinterpret_cast<float4_u*>(out + p) = zero;
+            __builtin_nontemporal_store(zero, reinterpret_cast<float4_u*>(out + p));
         } else {
             for (int64_t q = p; q < to; ++q) out[q] = 0.0f;
         }
@@ -743,7 +743,7 @@ __global__ void __launch_bounds__(kBlockThreads, 4) es_q8_vals_kernel(const Q8Ar
                         if (i >= n) i -= n;
                     }
                     if (idx + 4 <= n) {
-                        *reinterpret_cast<float4_u*>(out + idx) = v;
+                        __builtin_nontemporal_store(v, reinterpret_cast<float4_u*>(out + idx));   // out of the codes' way in the L2
                     } else {
 #pragma unroll
                         for (int j = 0; j < 4; ++j)
