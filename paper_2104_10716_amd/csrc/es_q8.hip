@@ -350,18 +350,22 @@ int es_spmm_q8_backward_vals(const int32_t* rowptr, const int32_t* colidx, const
 
 namespace {
 
-// The parts that the rows of X are cut into: two workgroups per compute unit in all, and four steps of each wave or more.
+// The parts that the rows of X are cut into: two workgroups per compute unit in all, and a step of each wave or more.
 struct GradPlan {
+    int MT, NT;                // tiles of the instruction per wave, along F and along H
     int64_t tiles_m, tiles, parts, part_rows;
 };
 
 GradPlan plan_grad(int64_t N, int32_t F, int32_t H, size_t workspace_bytes)
 {
     GradPlan p;
-    p.tiles_m = ((int64_t)F + kGradM - 1) / kGradM;
-    p.tiles = p.tiles_m * (((int64_t)H + kGradN - 1) / kGradN);
+    p.MT = F <= kGradTile ? 1 : F <= 2 * kGradTile ? 2 : 4;
+    p.NT = H <= kGradTile ? 1 : 2;
+    const int64_t m = p.MT * kGradTile, n = p.NT * kGradTile;
+    p.tiles_m = (F + m - 1) / m;
+    p.tiles = p.tiles_m * ((H + n - 1) / n);
     p.parts = 2 * kComputeUnits / p.tiles;
-    if (p.parts > N / (4 * kGradRows)) p.parts = N / (4 * kGradRows);
+    if (p.parts > N / kGradRows) p.parts = N / kGradRows;
     if (p.parts > kNumXcd) p.parts -= p.parts % kNumXcd;       // each XCD as many
     if (p.parts < 1) p.parts = 1;
     p.part_rows = ((N + p.parts - 1) / p.parts + kGradRows - 1) / kGradRows * kGradRows;
@@ -398,8 +402,11 @@ int es_q8_weight_grad(const int8_t* codes, int32_t ldq, const float* scale, cons
     const Q8Grad a = {codes, scale, G, join ? static_cast<float*>(workspace) : dW, N, F, H, ldq, ldg, join ? H : ldw,
                       (int32_t)p.tiles_m, (int32_t)p.tiles, p.part_rows, (int32_t)p.parts};
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if (H == 1) hipLaunchKernelGGL(es_q8_grad_kernel<true>, dim3((uint32_t)grid), dim3(kBlockThreads), 0, st, a);
-    else hipLaunchKernelGGL(es_q8_grad_kernel<false>, dim3((uint32_t)grid), dim3(kBlockThreads), 0, st, a);
+#define ES_GRAD(MT_, NT_)                                                                                            \
+    if (p.MT == MT_ && p.NT == NT_)                                                                                  \
+        hipLaunchKernelGGL((es_q8_grad_kernel<MT_, NT_>), dim3((uint32_t)grid), dim3(kBlockThreads), 0, st, a);
+    ES_GRAD(1, 1) ES_GRAD(1, 2) ES_GRAD(2, 1) ES_GRAD(2, 2) ES_GRAD(4, 1) ES_GRAD(4, 2)
+#undef ES_GRAD
     if (launched() != ES_OK) return ES_ERR_LAUNCH;
     if (!join) return ES_OK;
     uint32_t gj;

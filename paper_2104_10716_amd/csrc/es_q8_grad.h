@@ -9,7 +9,7 @@
 // A matrix instruction wants 8 rows r of one column i (or j) in a lane's registers, and in memory a row's columns lie
 // side by side.  No data has to be turned for that: a lane loads the same 4 columns of codes (2 of G) of 8 rows, and
 // registers number c of those loads are what the lane owes the c-th of 4 (2) tiles; which 32 columns
-// a tile then has, every fourth (second), is of no consequence until the result is stored.
+// a tile then has, every fourth (second), is of no consequence until the result is stored.  A narrow dW takes fewer tiles.
 #ifndef ES_SPMM_Q8_GRAD_H
 #define ES_SPMM_Q8_GRAD_H
 
@@ -29,19 +29,26 @@ struct Q8Grad {
     int32_t parts;
 };
 
-constexpr int kGradM = 128, kGradN = 64;                       // a wave's tile of dW: 4 x 2 tiles of the instruction
+constexpr int kGradTile = 32;                                  // rows and columns of dW of an instruction
 constexpr int kGradStep = 16;                                  // rows of X that an instruction sums
 constexpr int kGradRows = kGradStep * kWavesPerBlock;          // ... and a workgroup's four waves together
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef float float2_u __attribute__((ext_vector_type(2), aligned(4)));
 typedef float float4_u4 __attribute__((ext_vector_type(4), aligned(4)));
 
+// One load of MT codes or of NT numbers of G, at any alignment.
+template <int MT> struct GradCodes;
+template <> struct GradCodes<1> { typedef uint8_t type; };
+template <> struct GradCodes<2> { typedef uint16_t type; };
+template <> struct GradCodes<4> { typedef uint32_t type; };
+template <int NT> struct GradPair { typedef float type __attribute__((ext_vector_type(NT), aligned(4))); };
+
 // What a lane loads of 8 rows.
+template <int NT>
 struct GradRows {
     uint32_t code[8];
-    float2_u g[8];
+    float g[8][NT];
     float4_u4 scale[2];
 };
 
@@ -53,11 +60,12 @@ __device__ __forceinline__ uint32_t upper_halves(float low, float high)
 union GradFrag { uint32_t w[4]; bf16x8 v; };
 
 // The four waves of a workgroup take the part's steps in turn and add up their tiles in LDS, in their order.
-// SINGLE: G has one column, and so no pairs.
-template <bool SINGLE>
+// A wave's tile of dW is MT x NT tiles of the instruction.
+template <int MT, int NT>
 __global__ void __launch_bounds__(kBlockThreads, 2) es_q8_grad_kernel(const Q8Grad a)
 {
-    __shared__ float sums[2][kGradM * kGradN];
+    constexpr int M = MT * kGradTile, N = NT * kGradTile;
+    __shared__ float sums[2][M * N];
     const int lane = threadIdx.x & (kWaveSize - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n = lane & 31, half = lane >> 5;
     // the tiles of a part run on one XCD: they read the same rows
@@ -65,72 +73,76 @@ __global__ void __launch_bounds__(kBlockThreads, 2) es_q8_grad_kernel(const Q8Gr
     const uint32_t i = blockIdx.x / groups;
     const int32_t part = (int32_t)(i / a.tiles * groups + blockIdx.x % groups), tile = (int32_t)(i % a.tiles);
     if (part >= a.parts) return;
-    const int32_t m0 = tile % a.tiles_m * kGradM, n0 = tile / a.tiles_m * kGradN;
+    const int32_t m0 = tile % a.tiles_m * M, n0 = tile / a.tiles_m * N;
     const int64_t lo = part * a.part_rows, hi = min(a.N, lo + a.part_rows);
-    const int32_t cm = m0 + 4 * n, cn = n0 + 2 * n;
-    // Lanes behind the last column load the first ones; what they sum is not stored.  Bytes from the step's first row on:
+    const int32_t cm = m0 + MT * n, cn = n0 + NT * n;
+    // Lanes behind the last column load the first ones; what they sum is not stored.  A pair whose first column is the last one
+    // begins one before it: the second sum is that column's.  Bytes from the step's first row on:
     const uint32_t at_code = 8u * half * a.ldq + (cm < ((a.F + 15) & ~15) ? cm : 0);
-    const uint32_t at_g = 4u * (8u * half * a.ldg + (cn + 2 <= a.H ? cn : !SINGLE && cn < a.H ? a.H - 2 : 0));
-    const bool last = !SINGLE && cn + 1 == a.H;                // the pair ends with this lane's first column: its second sum
+    const uint32_t at_g = 4u * (8u * half * a.ldg + (cn + NT <= a.H ? cn : NT == 2 && cn < a.H ? a.H - 2 : 0));
 
-    f32x16 acc[4][2];
+    f32x16 acc[MT][NT];
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
+    for (int t = 0; t < MT; ++t)
 #pragma unroll
-        for (int s = 0; s < 2; ++s)
+        for (int s = 0; s < NT; ++s)
 #pragma unroll
             for (int j = 0; j < 16; ++j) acc[t][s][j] = 0.0f;
 
     // Addresses: those of the wave's rows, in scalar registers, and the lane's 32-bit offset.
-    auto load = [&](GradRows& q, int64_t r0) {
+    auto load = [&](GradRows<NT>& q, int64_t r0) {
         const char* code = reinterpret_cast<const char*>(a.codes) + r0 * a.ldq;
         const char* g = reinterpret_cast<const char*>(a.G) + r0 * a.ldg * 4;
 #pragma unroll
         for (int j = 0; j < 2; ++j) q.scale[j] = *reinterpret_cast<const float4_u4*>(a.scale + r0 + 4 * j + 8u * half);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            q.code[j] = *reinterpret_cast<const uint32_t*>(code + (int64_t)j * a.ldq + at_code);
-            const char* p = g + (int64_t)j * a.ldg * 4 + at_g;
-            if constexpr (SINGLE) { q.g[j].x = *reinterpret_cast<const float*>(p); q.g[j].y = 0.0f; }
-            else q.g[j] = *reinterpret_cast<const float2_u*>(p);
+            q.code[j] = *reinterpret_cast<const typename GradCodes<MT>::type*>(code + (int64_t)j * a.ldq + at_code);
+            const auto v = *reinterpret_cast<const typename GradPair<NT>::type*>(g + (int64_t)j * a.ldg * 4 + at_g);
+#pragma unroll
+            for (int s = 0; s < NT; ++s) q.g[j][s] = v[s];
         }
     };
-    auto load_end = [&](GradRows& q, int64_t r0) {             // fewer than 16 rows: zeros behind them
+    auto load_end = [&](GradRows<NT>& q, int64_t r0) {             // fewer than 16 rows: zeros behind them
         const int left = (int)(hi - r0) - 8 * half;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             q.code[j] = 0u;
-            q.scale[j / 4][j % 4] = q.g[j].x = q.g[j].y = 0.0f;
+            q.scale[j / 4][j % 4] = 0.0f;
+#pragma unroll
+            for (int s = 0; s < NT; ++s) q.g[j][s] = 0.0f;
             if (j < left) {
                 const int64_t r = r0 + 8 * half + j;
-                q.code[j] = *reinterpret_cast<const uint32_t*>(a.codes + (r0 + j) * a.ldq + at_code);
+                q.code[j] = *reinterpret_cast<const typename GradCodes<MT>::type*>(a.codes + (r0 + j) * a.ldq + at_code);
                 q.scale[j / 4][j % 4] = a.scale[r];
                 const float* p = reinterpret_cast<const float*>(reinterpret_cast<const char*>(a.G + (r0 + j) * a.ldg) + at_g);
-                q.g[j].x = p[0];
-                if constexpr (!SINGLE) q.g[j].y = p[1];
+#pragma unroll
+                for (int s = 0; s < NT; ++s) q.g[j][s] = p[s];
             }
         }
     };
-    auto multiply = [&](GradRows& q) {
+    auto multiply = [&](GradRows<NT>& q) {
         // what is loaded is first looked at here: the conversions stay behind the next step's loads
 #pragma unroll
-        for (int j = 0; j < 8; ++j) asm volatile("" : "+v"(q.code[j]), "+v"(q.g[j].x), "+v"(q.g[j].y));
+        for (int j = 0; j < 8; ++j) {
+            asm volatile("" : "+v"(q.code[j]), "+v"(q.scale[j / 4][j % 4]));
 #pragma unroll
-        for (int j = 0; j < 8; ++j) asm volatile("" : "+v"(q.scale[j / 4][j % 4]));
-        GradFrag x[4];
+            for (int s = 0; s < NT; ++s) asm volatile("" : "+v"(q.g[j][s]));
+        }
+        GradFrag x[MT];
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
+        for (int t = 0; t < MT; ++t)
 #pragma unroll
             for (int j = 0; j < 8; j += 2)
                 x[t].w[j / 2] = upper_halves((float)(int8_t)(q.code[j] >> (8 * t)), (float)(int8_t)(q.code[j + 1] >> (8 * t)));
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
+        for (int s = 0; s < NT; ++s) {
             GradFrag y[3];
 #pragma unroll
             for (int j = 0; j < 8; j += 2) {
                 float v[2];
 #pragma unroll
-                for (int u = 0; u < 2; ++u) v[u] = (s == 0 ? q.g[j + u].x : q.g[j + u].y) * q.scale[(j + u) / 4][(j + u) % 4];
+                for (int u = 0; u < 2; ++u) v[u] = q.g[j + u][s] * q.scale[(j + u) / 4][(j + u) % 4];
 #pragma unroll
                 for (int p = 0; p < 3; ++p) {
                     y[p].w[j / 2] = upper_halves(v[0], v[1]);
@@ -141,16 +153,16 @@ __global__ void __launch_bounds__(kBlockThreads, 2) es_q8_grad_kernel(const Q8Gr
 #pragma unroll
             for (int p = 0; p < 3; ++p)
 #pragma unroll
-                for (int t = 0; t < 4; ++t) acc[t][s] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[t].v, y[p].v, acc[t][s], 0, 0, 0);
+                for (int t = 0; t < MT; ++t) acc[t][s] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[t].v, y[p].v, acc[t][s], 0, 0, 0);
         }
     };
 
-    GradRows q;
+    GradRows<NT> q;
     const int64_t first = lo + wave * kGradStep, full = hi - first >= kGradStep ? (hi - first - kGradStep) / kGradRows + 1 : 0;
     if (full > 0) {
         load(q, first);
         for (int64_t s = 0; s < full; s += 2) {                // the next step's rows are requested before this one's are used
-            GradRows next;
+            GradRows<NT> next;
             load(next, first + min(s + 1, full - 1) * kGradRows);
             multiply(q);
             load(q, first + min(s + 2, full - 1) * kGradRows);
@@ -167,37 +179,39 @@ __global__ void __launch_bounds__(kBlockThreads, 2) es_q8_grad_kernel(const Q8Gr
     for (int round = 2; round >= 1; --round) {
         if (wave >= round && wave < 2 * round) {
 #pragma unroll
-            for (int t = 0; t < 4; ++t)
+            for (int t = 0; t < MT; ++t)
 #pragma unroll
-                for (int s = 0; s < 2; ++s)
+                for (int s = 0; s < NT; ++s)
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) sums[wave - round][((t * 2 + s) * 16 + j) * kWaveSize + lane] = acc[t][s][j];
+                    for (int j = 0; j < 16; ++j) sums[wave - round][((t * NT + s) * 16 + j) * kWaveSize + lane] = acc[t][s][j];
         }
         __syncthreads();
         if (wave < round) {
 #pragma unroll
-            for (int t = 0; t < 4; ++t)
+            for (int t = 0; t < MT; ++t)
 #pragma unroll
-                for (int s = 0; s < 2; ++s)
+                for (int s = 0; s < NT; ++s)
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) acc[t][s][j] += sums[wave][((t * 2 + s) * 16 + j) * kWaveSize + lane];
+                    for (int j = 0; j < 16; ++j) acc[t][s][j] += sums[wave][((t * NT + s) * 16 + j) * kWaveSize + lane];
         }
         __syncthreads();
     }
     if (wave > 0) return;
     float* out = a.dW + part * ((int64_t)a.F * a.ldw);
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
+    for (int t = 0; t < MT; ++t)
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
-            const int32_t f = m0 + 4 * (8 * (j / 4) + 4 * half + j % 4) + t;
+            const int32_t f = m0 + MT * (8 * (j / 4) + 4 * half + j % 4) + t;
             if (f >= a.F) continue;
             float* p = out + (int64_t)f * a.ldw + cn;
-            if (cn + 1 < a.H) {
-                float2_u v = {acc[t][0][j], acc[t][1][j]};
-                *reinterpret_cast<float2_u*>(p) = v;
+            if (cn + NT <= a.H) {
+                typename GradPair<NT>::type v;
+#pragma unroll
+                for (int s = 0; s < NT; ++s) v[s] = acc[t][s][j];
+                *reinterpret_cast<typename GradPair<NT>::type*>(p) = v;
             } else if (cn < a.H) {
-                p[0] = last ? acc[t][1][j] : acc[t][0][j];
+                p[0] = acc[t][NT - 1][j];
             }
         }
 }
