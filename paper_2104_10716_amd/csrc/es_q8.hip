@@ -50,16 +50,17 @@ bool grid_of(int64_t items, int64_t per_block, uint32_t* out)
 template <class T, int MAP>
 int launch_write(const Q8Write& a, hipStream_t st)
 {
-    const int64_t quads = ((int64_t)a.F + 15) / 16 * 4;
+    const int64_t loads = ((int64_t)a.F + 15) / 16 * (16 / Dense<T>::V);
     uint32_t grid;
 #define ES_WRITE(TEAM_, K_, UR_)                                                                                            \
-    if (quads <= (TEAM_) * (K_)) {                                                                                          \
+    if (loads <= (TEAM_) * (K_)) {                                                                                          \
         if (!grid_of(a.n, (int64_t)(kBlockThreads / (TEAM_)) * (UR_), &grid)) return ES_ERR_UNSUPPORTED;                    \
         hipLaunchKernelGGL((es_q8_write_kernel<T, TEAM_, K_, UR_, MAP>), dim3(grid), dim3(kBlockThreads), 0, st, a);        \
         return launched();                                                                                                  \
     }
     ES_WRITE(4, 1, 4) ES_WRITE(8, 1, 4) ES_WRITE(16, 1, 4) ES_WRITE(32, 1, 4) ES_WRITE(64, 1, 4)
-    ES_WRITE(64, 2, 2) ES_WRITE(64, 4, 1) ES_WRITE(64, 8, 1)
+    ES_WRITE(64, 2, 2) ES_WRITE(64, 3, 1) ES_WRITE(64, 4, 1)
+    if constexpr (Dense<T>::V == 4) { ES_WRITE(64, 8, 1) }
 #undef ES_WRITE
     if (!grid_of(a.n, 1, &grid)) return ES_ERR_UNSUPPORTED;
     hipLaunchKernelGGL((es_q8_write_wide_kernel<T, MAP>), dim3(grid), dim3(kBlockThreads), 0, st, a);
@@ -69,10 +70,10 @@ int launch_write(const Q8Write& a, hipStream_t st)
 template <class T>
 int launch_read(const Q8Read& a, hipStream_t st)
 {
-    const int64_t quads = ((int64_t)a.F + 3) / 4;
+    const int64_t stores = ((int64_t)a.F + Dense<T>::V - 1) / Dense<T>::V;
     uint32_t grid;
 #define ES_READ(TEAM_)                                                                                                      \
-    if (quads <= (TEAM_) || (TEAM_) == kWaveSize) {                                                                         \
+    if (stores <= (TEAM_) || (TEAM_) == kWaveSize) {                                                                        \
         if (!grid_of(a.n, (int64_t)(kBlockThreads / (TEAM_)) * 4, &grid)) return ES_ERR_UNSUPPORTED;                        \
         hipLaunchKernelGGL((es_q8_read_kernel<T, TEAM_, 4>), dim3(grid), dim3(kBlockThreads), 0, st, a);                    \
         return launched();                                                                                                  \

@@ -11,37 +11,41 @@
 
 namespace {
 
-// Four consecutive elements of a dense row at any alignment of the element's own size (one 64- or 128-bit
-// access: the HSA ABI runs the memory pipeline in unaligned-access mode).
-template <class T> struct Quad { typedef T type __attribute__((ext_vector_type(4), aligned(sizeof(T)))); };
-
+// 16 bytes of a dense row at any alignment of the element's own size: V elements (one 128-bit access: the HSA ABI runs
+// the memory pipeline in unaligned-access mode).
 template <class T>
-__device__ __forceinline__ void load_quad(const T* p, int left, float (&v)[4])
-{
-    if (left >= 4) {
-        const typename Quad<T>::type q = *reinterpret_cast<const typename Quad<T>::type*>(p);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = (float)q[j];
-    } else {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = j < left ? (float)p[j] : 0.0f;
-    }
-}
+struct Dense {
+    static constexpr int V = 16 / sizeof(T);
+    typedef T type __attribute__((ext_vector_type(V), aligned(sizeof(T))));
 
-template <class T>
-__device__ __forceinline__ void store_quad(T* p, int left, const float (&v)[4])
-{
-    if (left >= 4) {
-        typename Quad<T>::type q;
+    __device__ __forceinline__ static void load(const T* p, int left, float (&v)[V])
+    {
+        if (left >= V) {
+            const type q = *reinterpret_cast<const type*>(p);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) q[j] = (T)v[j];            // to nearest, ties to even
-        *reinterpret_cast<typename Quad<T>::type*>(p) = q;
-    } else {
+            for (int j = 0; j < V; ++j) v[j] = (float)q[j];
+        } else {
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (j < left) p[j] = (T)v[j];
+            for (int j = 0; j < V; ++j) v[j] = j < left ? (float)p[j] : 0.0f;
+        }
     }
-}
+    __device__ __forceinline__ static void store(T* p, int left, const float (&v)[V])
+    {
+        if (left >= V) {
+            type q;
+#pragma unroll
+            for (int j = 0; j < V; ++j) q[j] = (T)v[j];        // to nearest, ties to even
+            *reinterpret_cast<type*>(p) = q;
+        } else {
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+                if (j < left) p[j] = (T)v[j];
+        }
+    }
+};
+
+// V codes
+template <int V> struct Codes { typedef uint32_t type __attribute__((ext_vector_type(V / 4))); };
 
 // Scale of a row whose largest magnitude has these bits (as integers, magnitudes order like their values, infinity and
 // NaN above every number).  Below 127 * 2^-126 the scale would be subnormal: such a row is
@@ -55,31 +59,37 @@ __device__ __forceinline__ float q8_scale(uint32_t bits)
 
 __device__ __forceinline__ float q8_inverse(float scale) { return scale > 0.0f ? 1.0f / scale : 0.0f; }
 
-// The four codes of v as a word.  x * (1 / scale) is within 2e-5 of the quotient, so its nearest integer is the
+// The codes of v.  x * (1 / scale) is within 2e-5 of the quotient, so its nearest integer is the
 // quotient's or, next to a border, a neighbour of it; the remainder x - r * scale is a multiple of the
 // smaller of the operands' last places and below scale in size, so the fused multiply-add has it exactly,
 // and it says whether r is right.
-__device__ __forceinline__ uint32_t q8_codes(const float (&v)[4], float scale, float inv)
+template <int V>
+__device__ __forceinline__ typename Codes<V>::type q8_codes(const float (&v)[V], float scale, float inv)
 {
-    float r[4], e[4];
+    float r[V], e[V];
     float worst = 0.0f;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
+    for (int j = 0; j < V; ++j) {
         r[j] = rintf(v[j] * inv);
         e[j] = 2.0f * fmaf(-r[j], scale, v[j]);
         worst = fmaxf(worst, fabsf(e[j]));
     }
     if (worst >= scale) {                                      // a border, or a row held as zeros
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < V; ++j) {
             const float a = fabsf(e[j]);
             if (a > scale || (a == scale && ((int)r[j] & 1))) r[j] += copysignf(1.0f, e[j]);
         }
     }
-    uint32_t word = 0;
+    typename Codes<V>::type words;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) word |= ((uint32_t)(int)r[j] & 0xFFu) << (8 * j);
-    return scale > 0.0f ? word : 0u;                           // zeros for scale 0 and NaN
+    for (int w = 0; w < V / 4; ++w) {
+        uint32_t word = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) word |= ((uint32_t)(int)r[4 * w + j] & 0xFFu) << (8 * j);
+        words[w] = scale > 0.0f ? word : 0u;                   // zeros for scale 0 and NaN
+    }
+    return words;
 }
 
 enum { Q8_ALL = 0, Q8_SCANNED = 1, Q8_CLAIMED = 2 };           // how the table's rows are named
@@ -118,32 +128,35 @@ __device__ __forceinline__ int64_t q8_target(const Q8Write& a, int64_t i, int t)
     return later ? -1 : row;
 }
 
-// A team of TEAM lanes holds UR rows in registers, K quads of each per lane.  More rows at a time keep more bytes in flight.
+// A team of TEAM lanes holds UR rows in registers, K loads of each per lane.  More rows at a time keep more bytes in flight; the
+// rows are requested before it is known where, or whether, they go.
 template <class T, int TEAM, int K, int UR, int MAP>
 __global__ void __launch_bounds__(kBlockThreads) es_q8_write_kernel(const Q8Write a)
 {
+    constexpr int V = Dense<T>::V;
     const int t = threadIdx.x & (TEAM - 1);
     const int64_t i0 = ((int64_t)blockIdx.x * (kBlockThreads / TEAM) + threadIdx.x / TEAM) * UR;
     const int f16 = (a.F + 15) & ~15;
-    float v[UR][K][4];
+    float v[UR][K][V];
     int64_t row[UR];
 #pragma unroll
     for (int u = 0; u < UR; ++u) {
-        row[u] = i0 + u < a.n ? q8_target<MAP, TEAM>(a, i0 + u, t) : -1;
-        const T* x = static_cast<const T*>(a.X) + (row[u] < 0 ? 0 : i0 + u) * (int64_t)a.ldx;
+        const T* x = static_cast<const T*>(a.X) + min(i0 + u, a.n - 1) * (int64_t)a.ldx;
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            const int c = (k * TEAM + t) * 4;
-            load_quad(x + c, row[u] < 0 ? 0 : a.F - c, v[u][k]);
+            const int c = (k * TEAM + t) * V;
+            Dense<T>::load(x + c, a.F - c, v[u][k]);
         }
     }
+#pragma unroll
+    for (int u = 0; u < UR; ++u) row[u] = i0 + u < a.n ? q8_target<MAP, TEAM>(a, i0 + u, t) : -1;
 #pragma unroll
     for (int u = 0; u < UR; ++u) {
         uint32_t bits = 0;
 #pragma unroll
         for (int k = 0; k < K; ++k)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) bits = max(bits, __float_as_uint(v[u][k][j]) & 0x7FFFFFFFu);
+            for (int j = 0; j < V; ++j) bits = max(bits, __float_as_uint(v[u][k][j]) & 0x7FFFFFFFu);
         bits = team_reduce<TEAM>(bits, [](uint32_t x, uint32_t y) { return max(x, y); });
         if (row[u] < 0) continue;
         const float scale = q8_scale(bits);
@@ -151,8 +164,8 @@ __global__ void __launch_bounds__(kBlockThreads) es_q8_write_kernel(const Q8Writ
         int8_t* out = a.codes + row[u] * (int64_t)a.ldq;
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            const int c = (k * TEAM + t) * 4;
-            if (c < f16) *reinterpret_cast<uint32_t*>(out + c) = q8_codes(v[u][k], scale, inv);
+            const int c = (k * TEAM + t) * V;
+            if (c < f16) *reinterpret_cast<typename Codes<V>::type*>(out + c) = q8_codes(v[u][k], scale, inv);
         }
         if (t == 0)
             __hip_atomic_store(reinterpret_cast<uint32_t*>(a.scale) + row[u], __float_as_uint(scale), __ATOMIC_RELAXED,
@@ -164,6 +177,7 @@ __global__ void __launch_bounds__(kBlockThreads) es_q8_write_kernel(const Q8Writ
 template <class T, int MAP>
 __global__ void __launch_bounds__(kBlockThreads) es_q8_write_wide_kernel(const Q8Write a)
 {
+    constexpr int V = Dense<T>::V;
     __shared__ uint32_t part[kWavesPerBlock];
     const int64_t i = blockIdx.x;
     const int lane = threadIdx.x & (kWaveSize - 1), wave = threadIdx.x >> 6;
@@ -174,11 +188,11 @@ __global__ void __launch_bounds__(kBlockThreads) es_q8_write_wide_kernel(const Q
     const T* x = static_cast<const T*>(a.X) + i * (int64_t)a.ldx;
     const int64_t f16 = ((int64_t)a.F + 15) & ~(int64_t)15;
     uint32_t bits = 0;
-    float v[4];
-    for (int64_t c = threadIdx.x * 4; c < a.F; c += kBlockThreads * 4) {
-        load_quad(x + c, (int)min((int64_t)4, a.F - c), v);
+    float v[V];
+    for (int64_t c = threadIdx.x * V; c < a.F; c += kBlockThreads * V) {
+        Dense<T>::load(x + c, (int)min((int64_t)V, a.F - c), v);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) bits = max(bits, __float_as_uint(v[j]) & 0x7FFFFFFFu);
+        for (int j = 0; j < V; ++j) bits = max(bits, __float_as_uint(v[j]) & 0x7FFFFFFFu);
     }
     bits = team_reduce<kWaveSize>(bits, [](uint32_t p, uint32_t q) { return max(p, q); });
     if (lane == 0) part[wave] = bits;
@@ -187,9 +201,9 @@ __global__ void __launch_bounds__(kBlockThreads) es_q8_write_wide_kernel(const Q
     const float scale = q8_scale(bits);
     const float inv = q8_inverse(scale);
     int8_t* out = a.codes + row * (int64_t)a.ldq;
-    for (int64_t c = threadIdx.x * 4; c < f16; c += kBlockThreads * 4) {
-        load_quad(x + c, (int)max((int64_t)0, min((int64_t)4, a.F - c)), v);
-        *reinterpret_cast<uint32_t*>(out + c) = q8_codes(v, scale, inv);
+    for (int64_t c = threadIdx.x * V; c < f16; c += kBlockThreads * V) {
+        Dense<T>::load(x + c, (int)max((int64_t)0, min((int64_t)V, a.F - c)), v);
+        *reinterpret_cast<typename Codes<V>::type*>(out + c) = q8_codes(v, scale, inv);
     }
     if (threadIdx.x == 0)
         __hip_atomic_store(reinterpret_cast<uint32_t*>(a.scale) + row, __float_as_uint(scale), __ATOMIC_RELAXED,
@@ -220,10 +234,11 @@ struct Q8Read {
     int32_t F, ldq, ldy;
 };
 
-// Four codes per lane at a time: the stores, which are most of the bytes, are whole lines.
+// 16 bytes of Y per lane at a time: the stores, which are most of the bytes, are whole lines.
 template <class T, int TEAM, int UR>
 __global__ void __launch_bounds__(kBlockThreads) es_q8_read_kernel(const Q8Read a)
 {
+    constexpr int V = Dense<T>::V;
     const int t = threadIdx.x & (TEAM - 1);
     const int64_t i0 = ((int64_t)blockIdx.x * (kBlockThreads / TEAM) + threadIdx.x / TEAM) * UR;
     int64_t row[UR];
@@ -236,18 +251,20 @@ __global__ void __launch_bounds__(kBlockThreads) es_q8_read_kernel(const Q8Read 
     }
 #pragma unroll
     for (int u = 0; u < UR; ++u) scale[u] = row[u] < 0 ? 0.0f : a.scale[row[u]];
-    for (int64_t c = t * 4; c < a.F; c += TEAM * 4) {
-        uint32_t q[UR];
+    for (int64_t c = t * V; c < a.F; c += TEAM * V) {
+        typename Codes<V>::type q[UR];
 #pragma unroll
-        for (int u = 0; u < UR; ++u)
-            q[u] = row[u] < 0 ? 0u : *reinterpret_cast<const uint32_t*>(a.codes + row[u] * (int64_t)a.ldq + c);
+        for (int u = 0; u < UR; ++u) {
+            q[u] = 0u;
+            if (row[u] >= 0) q[u] = *reinterpret_cast<const typename Codes<V>::type*>(a.codes + row[u] * (int64_t)a.ldq + c);
+        }
 #pragma unroll
         for (int u = 0; u < UR; ++u) {
             if (i0 + u >= a.n) continue;
-            float v[4];
+            float v[V];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) v[j] = scale[u] * (float)(int8_t)(q[u] >> (8 * j));
-            store_quad(static_cast<T*>(a.Y) + (i0 + u) * (int64_t)a.ldy + c, (int)min((int64_t)4, a.F - c), v);
+            for (int j = 0; j < V; ++j) v[j] = scale[u] * (float)(int8_t)(q[u][j / 4] >> (8 * (j % 4)));
+            Dense<T>::store(static_cast<T*>(a.Y) + (i0 + u) * (int64_t)a.ldy + c, (int)min((int64_t)V, a.F - c), v);
         }
     }
 }
