@@ -454,7 +454,8 @@ int32_t es_q8_row_bytes(int32_t F);   /* 0 for F < 1 or F > 2^31 - 16 */
  *   rows   [n] int32 (device): row i of X becomes row rows[i] of the table; NULL: row i
  *          (n <= N).  An id outside [0, N) is skipped (a padded batch).  Where an id
  *          occurs more than once its last row is the one that is written.
- * Rows of the table that are not named keep their contents.
+ * Rows of the table that are not named keep their contents.  Calls that write the same
+ * rows must be ordered (same stream), as must those that read them.
  */
 int es_q8_write(const void* X, int32_t type, int64_t n, int32_t F, int32_t ldx,
                 const int32_t* rows, int64_t N, int8_t* codes, int32_t ldq, float* scale,
@@ -523,7 +524,9 @@ int es_spmm_q8_backward_vals(const int32_t* rowptr, const int32_t* colidx,
 /*
  * es_q8_weight_grad -- dW = X^T * G with X held as 8-bit rows: the weight gradient of a
  * dense layer Z = X * W (Equation 1's H * W) from the checkpoint of its input.
- *   G       N rows of H fp32, row stride ldg >= H: the gradient with respect to Z
+ *   G       N rows of H fp32, row stride ldg >= H: the gradient with respect to Z; meant
+ *           to hold finite values: an element of dW whose exact value is +-Inf may come
+ *           out as NaN.  ldg and ldq below 2^27.
  *   dW      F rows of H fp32, row stride ldw >= H, overwritten (zeros for N == 0)
  *   workspace  es_q8_weight_grad_workspace_bytes(N, F, H) bytes (0: none is of use),
  *           16-byte aligned; contents on entry are irrelevant, on return unspecified;

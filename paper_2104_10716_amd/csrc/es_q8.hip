@@ -47,6 +47,11 @@ bool grid_of(int64_t items, int64_t per_block, uint32_t* out)
     return true;
 }
 
+// Lanes to a row of so many 16-byte accesses, accesses per lane, and rows at a time: the fewest idle lanes.  233 k rows of 602
+// bf16 with 64 lanes throughout: written in 127 us and read in 100, this way 95 and 93; of 602 fp32: read in 188, 154.
+#define ES_TEAMS(X) X(4, 1, 4) X(8, 1, 4) X(16, 1, 4) X(32, 1, 4) X(16, 3, 2) X(64, 1, 4) X(16, 5, 1) X(32, 3, 2) X(64, 2, 2) \
+    X(32, 5, 1) X(64, 3, 1) X(64, 4, 1)
+
 template <class T, int MAP>
 int launch_write(const Q8Write& a, hipStream_t st)
 {
@@ -58,8 +63,7 @@ int launch_write(const Q8Write& a, hipStream_t st)
         hipLaunchKernelGGL((es_q8_write_kernel<T, TEAM_, K_, UR_, MAP>), dim3(grid), dim3(kBlockThreads), 0, st, a);        \
         return launched();                                                                                                  \
     }
-    ES_WRITE(4, 1, 4) ES_WRITE(8, 1, 4) ES_WRITE(16, 1, 4) ES_WRITE(32, 1, 4) ES_WRITE(64, 1, 4)
-    ES_WRITE(64, 2, 2) ES_WRITE(64, 3, 1) ES_WRITE(64, 4, 1)
+    ES_TEAMS(ES_WRITE)
     if constexpr (Dense<T>::V == 4) { ES_WRITE(64, 8, 1) }
 #undef ES_WRITE
     if (!grid_of(a.n, 1, &grid)) return ES_ERR_UNSUPPORTED;
@@ -72,13 +76,14 @@ int launch_read(const Q8Read& a, hipStream_t st)
 {
     const int64_t stores = ((int64_t)a.F + Dense<T>::V - 1) / Dense<T>::V;
     uint32_t grid;
-#define ES_READ(TEAM_)                                                                                                      \
-    if (stores <= (TEAM_) || (TEAM_) == kWaveSize) {                                                                        \
-        if (!grid_of(a.n, (int64_t)(kBlockThreads / (TEAM_)) * 4, &grid)) return ES_ERR_UNSUPPORTED;                        \
-        hipLaunchKernelGGL((es_q8_read_kernel<T, TEAM_, 4>), dim3(grid), dim3(kBlockThreads), 0, st, a);                    \
+#define ES_READ(TEAM_, K_, UR_)                                                                                             \
+    if (stores <= (TEAM_) * (K_) || (TEAM_) * (K_) == 256) {                                                                \
+        if (!grid_of(a.n, (int64_t)(kBlockThreads / (TEAM_)) * (UR_), &grid)) return ES_ERR_UNSUPPORTED;                    \
+        hipLaunchKernelGGL((es_q8_read_kernel<T, TEAM_, K_, UR_>), dim3(grid), dim3(kBlockThreads), 0, st, a);              \
         return launched();                                                                                                  \
     }
-    ES_READ(2) ES_READ(4) ES_READ(8) ES_READ(16) ES_READ(32) ES_READ(64)
+    ES_READ(2, 1, 4)
+    ES_TEAMS(ES_READ)
 #undef ES_READ
     return ES_ERR_UNSUPPORTED;
 }

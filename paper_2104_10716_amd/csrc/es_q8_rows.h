@@ -234,8 +234,8 @@ struct Q8Read {
     int32_t F, ldq, ldy;
 };
 
-// 16 bytes of Y per lane at a time: the stores, which are most of the bytes, are whole lines.
-template <class T, int TEAM, int UR>
+// 16 bytes of Y per lane and store: the stores are most of the bytes.  K loads of each of UR rows are in flight per lane.
+template <class T, int TEAM, int K, int UR>
 __global__ void __launch_bounds__(kBlockThreads) es_q8_read_kernel(const Q8Read a)
 {
     constexpr int V = Dense<T>::V;
@@ -251,20 +251,29 @@ __global__ void __launch_bounds__(kBlockThreads) es_q8_read_kernel(const Q8Read 
     }
 #pragma unroll
     for (int u = 0; u < UR; ++u) scale[u] = row[u] < 0 ? 0.0f : a.scale[row[u]];
-    for (int64_t c = t * V; c < a.F; c += TEAM * V) {
-        typename Codes<V>::type q[UR];
+    for (int64_t c0 = t * V; c0 - t * V < a.F; c0 += K * TEAM * V) {
+        typename Codes<V>::type q[UR][K];
 #pragma unroll
-        for (int u = 0; u < UR; ++u) {
-            q[u] = 0u;
-            if (row[u] >= 0) q[u] = *reinterpret_cast<const typename Codes<V>::type*>(a.codes + row[u] * (int64_t)a.ldq + c);
-        }
+        for (int u = 0; u < UR; ++u)
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                const int64_t c = c0 + k * TEAM * V;
+                q[u][k] = 0u;
+                if (row[u] >= 0 && c < a.F)
+                    q[u][k] = *reinterpret_cast<const typename Codes<V>::type*>(a.codes + row[u] * (int64_t)a.ldq + c);
+            }
 #pragma unroll
         for (int u = 0; u < UR; ++u) {
             if (i0 + u >= a.n) continue;
-            float v[V];
 #pragma unroll
-            for (int j = 0; j < V; ++j) v[j] = scale[u] * (float)(int8_t)(q[u][j / 4] >> (8 * (j % 4)));
-            Dense<T>::store(static_cast<T*>(a.Y) + (i0 + u) * (int64_t)a.ldy + c, (int)min((int64_t)V, a.F - c), v);
+            for (int k = 0; k < K; ++k) {
+                const int64_t c = c0 + k * TEAM * V;
+                if (c >= a.F) continue;
+                float v[V];
+#pragma unroll
+                for (int j = 0; j < V; ++j) v[j] = scale[u] * (float)(int8_t)(q[u][k][j / 4] >> (8 * (j % 4)));
+                Dense<T>::store(static_cast<T*>(a.Y) + (i0 + u) * (int64_t)a.ldy + c, (int)min((int64_t)V, a.F - c), v);
+            }
         }
     }
 }

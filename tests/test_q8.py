@@ -158,6 +158,33 @@ def test_python_refuses_what_it_cannot_read():
             es.es_q8_write(x, q, s)
 
 
+def test_no_kernel_of_8_bit_rows_spills(tmp_path):
+    """From the library's own metadata: every code object that is linked into it, one per source file."""
+    import os
+    import re
+    import subprocess
+    from paper_2104_10716_amd import build
+    llvm = "/opt/rocm/llvm/bin"
+    if not os.path.exists(f"{llvm}/clang-offload-bundler"):
+        pytest.skip("no LLVM tools")
+    es.load_library()
+    fat = str(tmp_path / "fat")
+    subprocess.run([f"{llvm}/llvm-objcopy", "--dump-section", f".hip_fatbin={fat}", build.LIB, os.devnull], check=True)
+    data, magic, kernels = open(fat, "rb").read(), b"__CLANG_OFFLOAD_BUNDLE__", {}
+    starts = [m.start() for m in re.finditer(re.escape(magic), data)]
+    for a, b in zip(starts, starts[1:] + [len(data)]):
+        bundle, code = str(tmp_path / "bundle"), str(tmp_path / "code")
+        open(bundle, "wb").write(data[a:b])
+        subprocess.run([f"{llvm}/clang-offload-bundler", "--type=o", "--unbundle", "--targets=hipv4-amdgcn-amd-amdhsa--gfx950",
+                        f"--input={bundle}", f"--output={code}"], check=True)
+        notes = subprocess.run([f"{llvm}/llvm-readelf", "--notes", code], check=True, capture_output=True, text=True).stdout
+        found = re.findall(r"\.name: +(_Z\w+kernel\w+)\n.*?\.private_segment_fixed_size: +(\d+)\n.*?\.vgpr_spill_count: +(\d+)\n",
+                           notes, re.S)
+        kernels.update({name: (int(scratch), int(spilled)) for name, scratch, spilled in found if "es_q8" in name})
+    assert len(kernels) > 100 and any("es_q8_grad_kernel" in k for k in kernels)
+    assert {k: v for k, v in kernels.items() if v != (0, 0)} == {}
+
+
 # ---- on the GPU -------------------------------------------------------------------------------
 def dev(a):
     import torch
@@ -328,6 +355,40 @@ def test_tables_beyond_32_bit_offsets():
     tol = (np.abs(a)[:, None] * np.abs(v[order])).sum(0) * (len(ids) + 5) * U
     near(Z[0].cpu().numpy(), want, tol, "far rows")
     assert bool((Z[1] == 0).all())
+
+
+@pytest.mark.gpu
+def test_tables_beyond_64_gib():
+    """Rows 16 KiB apart: the largest offset no longer fits 32 bits of 16-byte units."""
+    import torch
+    N, F = 4_200_000, 40
+    whole = torch.empty((N, 16_384), dtype=torch.int8, device="cuda:0")        # 69 GB, hardly any of it touched
+    codes, scale = whole[:, 16:16 + es.es_q8_row_bytes(F)], torch.zeros(N, device="cuda:0")
+    rng = np.random.default_rng(3)
+    ids = np.array([1, 7, 2 ** 22, N - 2, N - 1], dtype=np.int32)
+    X = rng.standard_normal((len(ids), F)).astype(np.float32)
+    q, s, v = quantise(X)
+    es.es_q8_write(dev(X), codes, scale, rows=dev(ids))
+    Y = torch.empty((len(ids), F), device="cuda:0")
+    es.es_q8_read(codes, scale, Y, rows=dev(ids))
+    np.testing.assert_array_equal(Y.cpu().numpy(), q.astype(np.float32) * s[:, None])
+    rowptr = np.zeros(N + 1, dtype=np.int32)
+    rowptr[N - 2:] = len(ids)                                  # row N - 3 gathers them
+    a = rng.standard_normal(len(ids)).astype(np.float32)
+    g = dev(rowptr), dev(ids)
+    for rows in (dev(np.array([N - 3, 0], np.int32)), dev(np.concatenate([np.full(600, N - 3), np.zeros(600)]).astype(np.int32))):
+        Z = torch.empty((rows.numel(), F), device="cuda:0")
+        for mode, W in (("full", 0), ("fastrand", 7)):
+            es.es_spmm_q8(*g, dev(a), codes, scale, Z, W, mode, rows=rows)
+            tol = (np.abs(a)[:, None] * np.abs(v)).sum(0) * (len(ids) + 5) * U
+            near(Z[0].cpu().numpy(), (a[:, None].astype(np.float64) * v).sum(0), tol, "far rows")
+            assert bool((Z[-1] == 0).all())
+    dY = torch.zeros((N, F), device="cuda:0")
+    row = rng.standard_normal(F).astype(np.float32)
+    dY[N - 3] = dev(row)
+    for mode, W in (("full", 0), ("bucket", 9), ("fastrand", 9)):
+        da = es.es_spmm_q8_backward_vals(*g, dY, codes, scale, torch.empty(len(ids), device="cuda:0"), W, mode)
+        near(da.cpu().numpy(), (v * row).sum(1), (np.abs(v) * np.abs(row)).sum(1) * (F + 6) * U, "far da")
 
 
 def graph(N, avg, seed, long_row=0, dense_row=None):
