@@ -88,11 +88,12 @@ def line_floor_bytes(N: int, nnz_kept: int, F: int, ldx: int, L: int) -> int:
 
 
 def kernel_source_hash() -> str:
-    """Hash of the kernel sources; profiles/traffic.json carries the hash it was measured at."""
+    """Hash of the fp32 products' kernel sources (what es_spmm.hip is made of); profiles/traffic.json carries the
+    hash it was measured at."""
     h = hashlib.sha256()
     src = os.path.join(ROOT, "paper_2104_10716_amd", "csrc")
     for name in sorted(os.listdir(src)):
-        if name.endswith((".h", ".hip")):
+        if name.endswith((".h", ".hip")) and not name.startswith(("es_q8", "es_lanes")):
             h.update(name.encode())
             h.update(open(os.path.join(src, name), "rb").read())
     return h.hexdigest()[:16]

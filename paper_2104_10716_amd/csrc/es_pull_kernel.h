@@ -30,6 +30,20 @@ namespace {
 // two compares, and the result is bit-reproducible.
 // ---------------------------------------------------------------------------
 
+// (a * b) mod n for a, b < n < 2^31: quotient estimated in double (off by at
+// most one), remainder fixed up in integers.
+__device__ __forceinline__ uint32_t mulmod31(uint32_t a, uint32_t b, uint32_t n)
+{
+    const uint64_t prod = (uint64_t)a * b;
+    const uint64_t q = (uint64_t)((double)a * (double)b / (double)n);
+    int64_t rem = (int64_t)(prod - q * n);
+    if (rem < 0) rem += n;
+    if (rem < 0) rem += n;
+    if (rem >= (int64_t)n) rem -= n;
+    if (rem >= (int64_t)n) rem -= n;
+    return (uint32_t)rem;
+}
+
 // Inverse of the row's FastRand multiplier modulo its length (extended Euclid;
 // the multiplier is coprime to n by construction).  One thread per row.
 __global__ void __launch_bounds__(kBlockThreads)

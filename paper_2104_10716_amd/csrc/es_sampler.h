@@ -36,20 +36,6 @@ __device__ __forceinline__ uint32_t fastrand_offset(uint64_t seed, int64_t row, 
     return (uint32_t)(splitmix64_output(seed, (uint64_t)row + 1u) >> 32) % n;
 }
 
-// (a * b) mod n for a, b < n < 2^31: quotient estimated in double (off by at
-// most one), remainder fixed up in integers.
-__device__ __forceinline__ uint32_t mulmod31(uint32_t a, uint32_t b, uint32_t n)
-{
-    const uint64_t prod = (uint64_t)a * b;
-    const uint64_t q = (uint64_t)((double)a * (double)b / (double)n);
-    int64_t rem = (int64_t)(prod - q * n);
-    if (rem < 0) rem += n;
-    if (rem < 0) rem += n;
-    if (rem >= (int64_t)n) rem -= n;
-    if (rem >= (int64_t)n) rem -= n;
-    return (uint32_t)rem;
-}
-
 struct RowSampler {
     uint32_t idx;    // entry number the next call returns
     uint32_t step;   // increment per call, already reduced mod n
