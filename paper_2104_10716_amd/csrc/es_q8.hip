@@ -122,6 +122,28 @@ int check_product(int64_t N, int64_t nnz, int32_t F, int32_t ldq, int32_t ld, in
     return ES_OK;
 }
 
+// Lanes to a row.  As few as cover its columns leave little to sum across lanes and the fewest lanes idle; half a wave
+// is done with a row sooner, which counts where rows are few, or long and of very different lengths (uniform ids, us with G or 4 lanes /
+// 32 / 64; m: mean kept):
+//  * 2700 rows, exact, F = 16, m = 5: 15.6 / 7.5 / 7.7, F = 64, m = 30: 18.9 / 10.4 / 9.3, m = 100: 45 / 12.1 / 10.5; 8000 rows: 15.6 /
+//    8.5 / 9.5, 19.5 / 13.9 / 12.5, 52 / 20 / 20; 20 k rows: 20 / 15.5 / 18, 33 / 27 / 27, 97 / 54 / 54
+//  * 60 k rows, m = 5: 23 / 25 / 37, F = 64, m = 30: 61 / 51 / 56, F = 128, FastRand, m = 100: 70 / 54 / 55
+//  * 233 k rows, F = 64, m = 30: 168 / 162 / 190, Bucket m = 24: 60 / 74 / 119, exact m = 490: 2401 / 1887 / 1934, F = 128: 2487 / 2184 /
+//    2223, FastRand m = 200: 545 / 485 / 453, Bucket m = 32: 115 / 133 / 134, F = 256, m = 490: 4360 / 4402 / 4496
+//  * 700 k rows, F = 64, m = 30: 589 / 628 / 693, F = 19, Bucket m = 60: 645 / 614 / 628, F = 128, m = 60: 1177 / 1236 / 1259, FastRand
+//    m = 150: 1658 / 1544 / 1456; 2.45 M, F = 128, FastRand m = 50: 1359 / 1519 / 1505
+// The edge gradient: 2700 rows, F = 64, m = 30: 20 / 9.7 / 8.0; 20 k: 28 / 22 / 21; 233 k, F = 64, m = 100: 542 / 401 / 425, F = 128, m = 5:
+// 67 / 118 / 191.
+int pick_team(int G, int64_t n_rows, double mean)
+{
+    const int least = G < 4 ? 4 : G;
+    if (n_rows <= 4096) return kWaveSize;
+    if (n_rows <= 24'576) return G < 32 ? 32 : G;
+    if (G <= 8 && mean >= 56.0 && (G <= 4 || n_rows <= 300'000 || mean >= 150.0)) return 32;
+    if (G <= 8 && mean >= 28.0 && n_rows <= 98'304) return 32;
+    return least;
+}
+
 // Everything the host decides about one product on 8-bit rows.
 struct Q8Plan {
     int G;                     // lanes per row of codes
@@ -144,12 +166,14 @@ void plan_rows(Q8Plan& p, int64_t n_rows, double mean, int64_t Wk)
     // Rows per wave: the more, the more alike are those that run side by side; but every SIMD wants some waves.
     const int side = kWaveSize / p.team;                       // rows side by side
     p.wave_rows = 64;
-    while (p.wave_rows > side && p.wave_rows > 4 && n_rows / p.wave_rows < 8 * 4 * kComputeUnits) p.wave_rows /= 2;
+    while (p.wave_rows > side && n_rows / p.wave_rows < 8 * 4 * kComputeUnits) p.wave_rows /= 2;
     // a lane retires a batch of entries in some 1.5 us; a row should not take it a tenth of the launch
     const double us = mean * (double)n_rows * (double)(p.slices * (p.G * 16 + 12)) / 5.0e6;
-    double k = kQ8Batch * 0.07 * us;
+    const double side_by_side = (double)p.team / (double)p.G;  // entries of a row
+    double k = side_by_side * kQ8Batch * 0.07 * us;
     if (k < 4.0 * mean) k = 4.0 * mean;
-    p.long_k = k < 64.0 ? 64 : k > 1.0e9 ? 1000000000 : (int32_t)k;
+    const double least = 64.0 * (side_by_side < 8.0 ? side_by_side : 8.0);
+    p.long_k = k < least ? (int32_t)least : k > 1.0e9 ? 1000000000 : (int32_t)k;
     if (p.random) p.long_k = INT32_MAX;                        // W bounds them
     p.long_blocks = Wk > p.long_k ? (n_rows + kQ8ScanRows - 1) / kQ8ScanRows * kQ8Share : 0;
     p.nblocks = (n_rows + kWavesPerBlock * p.wave_rows - 1) / (kWavesPerBlock * p.wave_rows);
@@ -182,7 +206,7 @@ Q8Plan plan_q8(int64_t N, int64_t nnz, int32_t F, int32_t W, int32_t mode, int64
         p.piece = p.long_k = INT32_MAX;
         return p;
     }
-    p.team = p.G < 4 ? 4 : p.G;
+    p.team = pick_team(p.G, n_rows, mean);
     plan_rows(p, n_rows, mean, Wk);
     int64_t piece = 1024;
     while (piece * 8192 < nnz) piece *= 2;
@@ -200,7 +224,7 @@ Q8Plan plan_vals(int64_t N, int64_t nnz, int32_t F, int32_t W, int32_t mode)
     const int64_t Wk = mode == ES_FULL ? INT32_MAX : W;
     double mean = (double)nnz / (double)N;
     if (mean > (double)Wk) mean = (double)Wk;
-    p.team = p.G < 4 ? 4 : p.G;
+    p.team = pick_team(p.G, N, mean);
     p.random = mode == ES_FASTRAND && W <= kQ8MostRandom;
     // FastRand: a team's kept entries wait in LDS, which holds 64 of them for each of four rows side by side, or 1024 of one
     if (p.random) p.team = p.G <= 16 && W <= 64 ? 16 : kWaveSize;
@@ -224,13 +248,16 @@ int launch_q8(const Q8Args& a, const Q8Plan& p, hipStream_t st)
         }
         return launched();
     }
-#define ES_Q8(G_)                                                                                              \
-    case G_:                                                                                                   \
-        if (p.long_blocks) hipLaunchKernelGGL((es_q8_spmm_kernel<G_, true, WIDE>), grid, block, 0, st, a);     \
-        else hipLaunchKernelGGL((es_q8_spmm_kernel<G_, false, WIDE>), grid, block, 0, st, a);                  \
-        break;
+#define ES_SPMM(G_, TEAM_)                                                                                     \
+    if (p.team == (TEAM_)) {                                                                                   \
+        if (p.long_blocks) hipLaunchKernelGGL((es_q8_spmm_kernel<G_, TEAM_, true, WIDE>), grid, block, 0, st, a);  \
+        else hipLaunchKernelGGL((es_q8_spmm_kernel<G_, TEAM_, false, WIDE>), grid, block, 0, st, a);           \
+        break;                                                                                                 \
+    }
+#define ES_Q8(G_) case G_: ES_SPMM(G_, (G_) < 4 ? 4 : G_) ES_SPMM(G_, 32) ES_SPMM(G_, 64) break;
     switch (p.G) { ES_Q8(1) ES_Q8(2) ES_Q8(4) ES_Q8(8) ES_Q8(16) }
 #undef ES_Q8
+#undef ES_SPMM
     if (launched() != ES_OK) return ES_ERR_LAUNCH;
     if (p.pieces) {
         hipLaunchKernelGGL(es_q8_join_kernel, dim3((uint32_t)((a.n_rows + kQ8ScanRows - 1) / kQ8ScanRows)), block, 0, st, a);
@@ -243,20 +270,28 @@ template <bool WIDE>
 int launch_vals(const Q8Args& a, const Q8Plan& p, hipStream_t st)
 {
     const dim3 grid((uint32_t)p.grid_x), block(kBlockThreads);
+    const int kind = p.random ? Q8_RANDOM : p.long_blocks ? Q8_LONG : Q8_PREFIX;
     if (a.mode == ES_FASTRAND && !p.random) {
         hipLaunchKernelGGL(es_q8_zero_kernel, dim3(8 * kComputeUnits), block, 0, st, a);
         if (launched() != ES_OK) return ES_ERR_LAUNCH;
     }
-#define ES_VALS(G_, TEAM_, KIND_) hipLaunchKernelGGL((es_q8_vals_kernel<G_, TEAM_, KIND_, WIDE>), grid, block, 0, st, a)
-#define ES_Q8(G_)                                                                                              \
-    case G_:                                                                                                   \
-        if (p.random && p.team == 64) ES_VALS(G_, 64, Q8_RANDOM);                                              \
-        else if (p.random) ES_VALS(G_, (G_) <= 16 ? 16 : 64, Q8_RANDOM);                                        \
-        else if (p.long_blocks) ES_VALS(G_, (G_) < 4 ? 4 : G_, Q8_LONG);                                       \
-        else ES_VALS(G_, (G_) < 4 ? 4 : G_, Q8_PREFIX);                                                        \
+#define ES_VALS(G_, TEAM_, KIND_)                                                                                 \
+    if (p.team == (TEAM_) && kind == KIND_) {                                                                     \
+        hipLaunchKernelGGL((es_q8_vals_kernel<G_, TEAM_, KIND_, WIDE>), grid, block, 0, st, a);                   \
+        break;                                                                                                    \
+    }
+#define ES_TEAM(G_, TEAM_) ES_VALS(G_, TEAM_, Q8_PREFIX) ES_VALS(G_, TEAM_, Q8_LONG)
+#define ES_Q8(G_)                                                                                                 \
+    case G_:                                                                                                      \
+        ES_TEAM(G_, (G_) < 4 ? 4 : G_)                                                                            \
+        if constexpr ((G_) < 32) { ES_TEAM(G_, 32) }                                                              \
+        if constexpr ((G_) < 64) { ES_TEAM(G_, 64) }                                                              \
+        if constexpr ((G_) <= 16) { ES_VALS(G_, 16, Q8_RANDOM) }                                                  \
+        ES_VALS(G_, 64, Q8_RANDOM)                                                                                \
         break;
     switch (p.G) { ES_Q8(1) ES_Q8(2) ES_Q8(4) ES_Q8(8) ES_Q8(16) ES_Q8(32) ES_Q8(64) }
 #undef ES_Q8
+#undef ES_TEAM
 #undef ES_VALS
     return launched();
 }

@@ -138,20 +138,28 @@ __device__ __forceinline__ void q8_tile(const Q8Args& a, RowSampler& s, int t, i
     wave_lds_fence();
 }
 
-// Sums the lanes of a wave that are G, 2 G, ... apart.  Across its halves and the pairs of its rows of 16 lanes a
+// Sums the lanes of a team that are G, 2 G, ... apart.  Across the halves of a wave and the pairs of its rows of 16 lanes a
 // register swap leaves each side half of the columns, so that what is left to sum halves each time; inside 16 lanes
-// rotations add the rest.  Afterwards acc[0 .. 4) are this lane's columns from `first` on.
-template <int G>
+// rotations add the rest.  Afterwards acc[0 .. COLS) are this lane's columns from `first` on.
+template <int G, int TEAM>
 struct Q8Sum {
-    static constexpr int COLS = 4;
-    static_assert(G <= 16, "a chunk of columns lies inside 16 lanes");
-    __device__ __forceinline__ static int first(int lane) { return (lane >> 5) * 8 + (lane >> 4 & 1) * 4; }
+    static constexpr int COLS = TEAM == 64 ? 4 : TEAM == 32 ? 8 : 16;
+    static_assert(G <= 16 && TEAM >= 16, "a chunk of columns lies inside 16 lanes");
+    __device__ __forceinline__ static int first(int lane)
+    {
+        return TEAM == 64 ? (lane >> 5) * 8 + (lane >> 4 & 1) * 4 : TEAM == 32 ? (lane >> 4 & 1) * 8 : 0;
+    }
     __device__ __forceinline__ static void run(float (&acc)[kQ8Cols])
     {
+        if constexpr (TEAM == 64) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) { lane_swap<false>(acc[j], acc[j + 8]); acc[j] += acc[j + 8]; }
+            for (int j = 0; j < 8; ++j) { lane_swap<false>(acc[j], acc[j + 8]); acc[j] += acc[j + 8]; }
+        }
+        if constexpr (TEAM >= 32) {
+            constexpr int H = TEAM == 64 ? 4 : 8;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) { lane_swap<true>(acc[j], acc[j + 4]); acc[j] += acc[j + 4]; }
+            for (int j = 0; j < H; ++j) { lane_swap<true>(acc[j], acc[j + H]); acc[j] += acc[j + H]; }
+        }
 #pragma unroll
         for (int j = 0; j < COLS; ++j) {
             if constexpr (G <= 8) acc[j] += dpp_move<0x128>(acc[j]);               // row_ror:8
@@ -183,7 +191,7 @@ __device__ __forceinline__ void q8_block_sum(const Q8Args& a, const Q8Row& w, in
                                              uint2* lds, float (&acc)[kQ8Cols])
 {
     constexpr int E = kWaveSize / G;
-    using Sum = Q8Sum<G>;
+    using Sum = Q8Sum<G, kWaveSize>;
     const int lane = threadIdx.x & (kWaveSize - 1), wave = threadIdx.x >> 6;
     uint2* tile = lds + wave * kQ8Tile;
 #pragma unroll
@@ -293,7 +301,7 @@ struct Q8Kept {
 __device__ __forceinline__ int q8_rank(int k, int lane, int rows)
 {
     int rank = 0;
-    for (int j0 = 0; j0 < rows; j0 += 4)                       // rows is a multiple of 4
+    for (int j0 = 0; j0 < rows; j0 += 4)                       // lanes behind the rows have k = 0, and come behind any row
 #pragma unroll
         for (int j = j0; j < j0 + 4; ++j) {
             const int other = __builtin_amdgcn_readlane(k, j);
@@ -345,13 +353,14 @@ __device__ __forceinline__ void q8_team_sum(float (&acc)[kQ8Cols])
 
 // The product.  The leading workgroups take the long rows, whose waves would run long after the rest of the
 // launch: 16 of them share those among 1024 rows.  The rest take wave_rows rows per wave, each XCD a contiguous range of
-// rows: TEAM lanes to a row, 64 / TEAM rows side by side, TEAM / G entries of each at once, so that wide rows
-// need no sum across lanes.
+// rows: TEAM lanes to a row, 64 / TEAM rows side by side, TEAM / G entries of each at once.  TEAM is G, or 4, so that
+// there is nothing, or little, to sum across lanes; or a whole wave, where rows are too few to fill the chip and
+// what counts is how soon the longest is done.
 // LONG: there may be long rows (a kernel of its own without them keeps its registers).
-template <int G, bool LONG, bool WIDE>
+template <int G, int TEAM, bool LONG, bool WIDE>
 __global__ void __launch_bounds__(kBlockThreads, 5) es_q8_spmm_kernel(const Q8Args a)
 {
-    constexpr int TEAM = G < 4 ? 4 : G, ROWS = kWaveSize / TEAM;
+    constexpr int ROWS = kWaveSize / TEAM;
     constexpr int T = 4 * TEAM;                                // entries of a row staged at a time
     static_assert(T * ROWS == kQ8Tile, "");
     constexpr int ROW_SLOTS = T + 2;                           // and two of padding: the rows' entry j is in different banks
@@ -376,7 +385,7 @@ __global__ void __launch_bounds__(kBlockThreads, 5) es_q8_spmm_kernel(const Q8Ar
                 q8_piece_slots(a, w, piece, t0, count);
                 q8_block_sum<G, WIDE>(a, w, t0, count, codes, lds, acc);
                 if (wave == 0 && (lane & 15) < G) {
-                    const int c = c0 + Q8Sum<G>::first(lane);
+                    const int c = c0 + Q8Sum<G, kWaveSize>::first(lane);
                     if (w.k <= a.piece) {
                         q8_store(a.Y + i * (int64_t)a.ldy, c, a.F, acc, row_factor(a.norm, w.n, w.k));
                     } else {
@@ -409,24 +418,33 @@ __global__ void __launch_bounds__(kBlockThreads, 5) es_q8_spmm_kernel(const Q8Ar
         const int most = __builtin_amdgcn_readfirstlane(w.k), spare = __builtin_amdgcn_readfirstlane(w.base);
         for (int t0 = 0; t0 < most; t0 += T)
             q8_tile<G, TEAM, WIDE>(a, s, t, w.k - t0, min(most - t0, T), w.base, spare, tile, codes, acc);
-        q8_team_sum<G, TEAM>(acc);
-        // through LDS, so that a store instruction writes whole lines: lane t has the row's quads t, t + TEAM, ...
-        float* out = reinterpret_cast<float*>(own) + rs * (G * kQ8Cols);
-        if (t < G) {
-#pragma unroll
-            for (int j = 0; j < kQ8Cols; j += 4)
-                *reinterpret_cast<float4*>(out + l * kQ8Cols + j) = make_float4(acc[j], acc[j + 1], acc[j + 2], acc[j + 3]);
-        }
-        wave_lds_fence();
         const float f = row_factor(a.norm, w.n, w.k);
+        float* y = a.Y + (first_row + w.place) * (int64_t)a.ldy;
+        if constexpr (TEAM > G && TEAM >= 16) {
+            using Sum = Q8Sum<G, TEAM>;
+            Sum::run(acc);
+            if (w.place >= 0 && (lane & 15) < G) {
 #pragma unroll
-        for (int q = 0; q < 4 * G; q += TEAM) {
-            const float4 v = *reinterpret_cast<const float4*>(out + (q + t) * 4);
-            const float v4[4] = {v.x, v.y, v.z, v.w};
-            if (w.place >= 0)
-                q8_store(a.Y + (first_row + w.place) * (int64_t)a.ldy, blockIdx.y * G * kQ8Cols + (q + t) * 4, a.F, v4, f);
+                for (int j = 0; j < Sum::COLS; j += 4) q8_store(y, c0 + Sum::first(lane) + j, a.F, acc + j, f);
+            }
+        } else {
+            q8_team_sum<G, TEAM>(acc);
+            // through LDS, so that a store instruction writes whole lines: lane t has the row's quads t, t + TEAM, ...
+            float* out = reinterpret_cast<float*>(own) + rs * (G * kQ8Cols);
+            if (t < G) {
+#pragma unroll
+                for (int j = 0; j < kQ8Cols; j += 4)
+                    *reinterpret_cast<float4*>(out + l * kQ8Cols + j) = make_float4(acc[j], acc[j + 1], acc[j + 2], acc[j + 3]);
+            }
+            wave_lds_fence();
+#pragma unroll
+            for (int q = 0; q < 4 * G; q += TEAM) {
+                const float4 v = *reinterpret_cast<const float4*>(out + (q + t) * 4);
+                const float v4[4] = {v.x, v.y, v.z, v.w};
+                if (w.place >= 0) q8_store(y, blockIdx.y * G * kQ8Cols + (q + t) * 4, a.F, v4, f);
+            }
+            wave_lds_fence();
         }
-        wave_lds_fence();
     }
 }
 
@@ -482,7 +500,7 @@ __device__ __forceinline__ int32_t q8_few_length(const Q8Args& a, int32_t k)
 template <int G, bool WIDE>
 __global__ void __launch_bounds__(kBlockThreads) es_q8_few_kernel(const Q8Args a)
 {
-    using Sum = Q8Sum<G>;
+    using Sum = Q8Sum<G, kWaveSize>;
     __shared__ uint2 lds[kQ8Lds];
     const int lane = threadIdx.x & (kWaveSize - 1), wave = threadIdx.x >> 6;
     const int c0 = (blockIdx.y * G + (lane & (G - 1))) * kQ8Cols;
