@@ -540,6 +540,43 @@ def test_edge_gradient_on_row_lengths(N, avg, long_row):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("N,avg,long_row", [(3000, 6, 2900), (9000, 6, 7000), (26_000, 4, 25_000), (26_000, 60, 3000), (120_000, 3, 9000)])
+@pytest.mark.parametrize("F", [8, 20, 41, 100, 250])
+def test_every_share_of_a_wave(N, avg, long_row, F):
+    """Both products where a row is a whole wave's, half a wave's, and that of as few lanes as cover its columns."""
+    import oracle
+    import torch
+    from scipy.sparse import csr_matrix
+    rowptr, colidx = graph(N, avg, F, long_row)
+    rng = np.random.default_rng(N + F)
+    vals = rng.standard_normal(colidx.size).astype(np.float32)
+    dY = rng.standard_normal((N, F)).astype(np.float32)
+    X = rng.standard_normal((N, F)).astype(np.float32) * np.exp(rng.uniform(-3, 3, (N, 1))).astype(np.float32)
+    codes, scale, q, s, v = filled(X)
+    rows = np.repeat(np.arange(N), np.diff(rowptr))
+    d = dev(rowptr), dev(colidx)
+    for mode, W, seed in (("full", 0, 0), ("bucket", 24, 0), ("fastrand", 50, 9)):
+        keep = np.ones(colidx.size, bool)
+        if mode != "full":
+            pos, cnt = oracle.kept(rowptr, W, mode, seed)
+            keep[:] = False
+            keep[pos[np.arange(pos.shape[1])[None, :] < cnt[:, None]]] = True
+        k = np.add.reduceat(np.concatenate([keep, [False]]).astype(np.int64), rowptr[:-1]) * (np.diff(rowptr) > 0)
+        A = csr_matrix((np.where(keep, vals, 0).astype(np.float64), colidx, rowptr), shape=(N, N))
+        B = csr_matrix((np.abs(A.data), colidx, rowptr), shape=(N, N))
+        Y = es.es_spmm_q8(*d, dev(vals), codes, scale, torch.full((N, F), float("nan"), device="cuda:0"), W, mode, seed)
+        near(Y.cpu().numpy(), A @ v, (B @ np.abs(v)) * ((k + 5) * U)[:, None], f"{mode} {W}")
+        da = es.es_spmm_q8_backward_vals(*d, dev(dY), codes, scale, torch.full((colidx.size,), float("nan"), device="cuda:0"),
+                                         W, mode, seed)
+        want, tol = np.zeros(colidx.size), np.zeros(colidx.size)
+        for lo in range(0, colidx.size, 100_000):
+            e = slice(lo, lo + 100_000)
+            x, g = v[colidx[e]], dY[rows[e]].astype(np.float64)
+            want[e], tol[e] = (x * g).sum(1) * keep[e], (np.abs(x) * np.abs(g)).sum(1) * keep[e] * (F + 6) * U
+        near(da.cpu().numpy(), want, tol, f"da {mode} {W}")
+
+
+@pytest.mark.gpu
 def test_edge_gradient_against_differences():
     """The product is linear in the values, so a central difference of L = <dY, Y> has no truncation error, only the
     product's own rounding: two evaluations, each off by at most its tolerance, over a step of 2 h."""
