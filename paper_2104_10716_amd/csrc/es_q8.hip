@@ -144,6 +144,20 @@ int pick_team(int G, int64_t n_rows, double mean)
     return least;
 }
 
+// The same for the edge gradient of FastRand, whose kept entries wait in LDS: 256 of a row with 16 lanes, 512 with 32, 1024 with 64.
+// The wider the sample, the more its rows differ in length.  16 / 32 / 64 lanes, us (m: mean of the whole row):
+//  * 2700 rows, m = 14, F = 100, W = 100: 13.5 / 9.4 / 8.5; 8000 rows, m = 5, F = 16, W = 50: 7.3 / 7.0 / 8.2, m = 30, F = 128, W = 200: 26 / 19 / 15
+//  * 60 k rows, m = 5, F = 128, W = 50: 33 / 35 / 46, m = 14, F = 100, W = 100: 50 / 48 / 60, m = 100, F = 128, W = 250: 130 / 97 / 90; F = 300,
+//    m = 30, W = 16: - / 61 / 71, F = 400, W = 500: - / 248 / 203
+//  * 233 k rows, m = 5, F = 128, W = 50: 94 / 114 / 160, m = 30, W = 200: 167 / 160 / 198, m = 100, W = 250: 315 / 304 / 315; F = 300, W = 16: - / 228 / 280,
+//    F = 400, W = 500: - / 593 / 569; 700 k, m = 14, F = 100, W = 100: 416 / 522 / 793, m = 30, F = 128, W = 200: 461 / 485 / 625
+int pick_random_team(int G, int64_t n_rows, int32_t W)
+{
+    const bool many = n_rows > 98'304;
+    if (G > 32 || n_rows <= 4096 || W > 384 || (!many && W > (G <= 16 ? 224 : 127))) return kWaveSize;
+    return G <= 16 && W <= 256 && (many || (W <= 64 && n_rows > 12'288)) ? 16 : 32;
+}
+
 // Everything the host decides about one product on 8-bit rows.
 struct Q8Plan {
     int G;                     // lanes per row of codes
@@ -163,9 +177,11 @@ constexpr int64_t kFewRows = 512;
 // Rows to waves, and which rows are long, for rows that keep `mean` entries, at most Wk.
 void plan_rows(Q8Plan& p, int64_t n_rows, double mean, int64_t Wk)
 {
-    // Rows per wave: the more, the more alike are those that run side by side; but every SIMD wants some waves.
+    // Rows per wave: the more, the more alike are those that run side by side; but every SIMD wants some waves, and long rows in
+    // a wave's own order stray further from their neighbours' codes.  32 / 64: 2.45 M rows, F = 128, FastRand of 64 1301 / 1360 us, 2.06 M,
+    // F = 96, mean 4.6 468 / 455; the edge gradient, 544 k, F = 102, mean 41 533 / 549, 1.2 M, F = 48, mean 16 551 / 522.
     const int side = kWaveSize / p.team;                       // rows side by side
-    p.wave_rows = 64;
+    p.wave_rows = mean >= 24.0 ? 32 : 64;
     while (p.wave_rows > side && n_rows / p.wave_rows < 8 * 4 * kComputeUnits) p.wave_rows /= 2;
     // a lane retires a batch of entries in some 1.5 us; a row should not take it a tenth of the launch
     const double us = mean * (double)n_rows * (double)(p.slices * (p.G * 16 + 12)) / 5.0e6;
@@ -226,8 +242,7 @@ Q8Plan plan_vals(int64_t N, int64_t nnz, int32_t F, int32_t W, int32_t mode)
     if (mean > (double)Wk) mean = (double)Wk;
     p.team = pick_team(p.G, N, mean);
     p.random = mode == ES_FASTRAND && W <= kQ8MostRandom;
-    // FastRand: a team's kept entries wait in LDS, which holds 64 of them for each of four rows side by side, or 1024 of one
-    if (p.random) p.team = p.G <= 16 && W <= 64 ? 16 : kWaveSize;
+    if (p.random) p.team = pick_random_team(p.G, N, W);
     plan_rows(p, N, mean < 1.0 ? 1.0 : mean, p.random ? 0 : Wk);
     p.piece = 1024;                                            // each entry is for itself: pieces need no room and no join
     return p;
@@ -287,6 +302,7 @@ int launch_vals(const Q8Args& a, const Q8Plan& p, hipStream_t st)
         if constexpr ((G_) < 32) { ES_TEAM(G_, 32) }                                                              \
         if constexpr ((G_) < 64) { ES_TEAM(G_, 64) }                                                              \
         if constexpr ((G_) <= 16) { ES_VALS(G_, 16, Q8_RANDOM) }                                                  \
+        if constexpr ((G_) <= 32) { ES_VALS(G_, 32, Q8_RANDOM) }                                                  \
         ES_VALS(G_, 64, Q8_RANDOM)                                                                                \
         break;
     switch (p.G) { ES_Q8(1) ES_Q8(2) ES_Q8(4) ES_Q8(8) ES_Q8(16) ES_Q8(32) ES_Q8(64) }

@@ -555,7 +555,15 @@ __device__ __forceinline__ void q8_load_dy(const Q8Args& a, int64_t r, int c, fl
     }
 }
 
-// One tile of a row: TEAM lanes stage up to 4 TEAM entries, lane t those of slots t, t + TEAM, ...; edge slot e then takes the
+// The first slot of lane t of a team, whose next ones are TEAM apart: the edge slots (G lanes each) have the first TEAM / G
+// slots, then those behind them, so that a short row keeps all of them busy.
+template <int G, int TEAM>
+__device__ __forceinline__ int q8_slot(int t)
+{
+    return (t & (G - 1)) * (TEAM / G) + t / G;
+}
+
+// One tile of a row: TEAM lanes stage up to 4 TEAM entries, from slot `first` = q8_slot of the lane on; edge slot e then takes the
 // entries of the lanes e G .. e G + G - 1, one after the other: G lanes multiply, their shares meet in registers, and the lane that
 // staged an entry keeps its product.  `most`, `spare` as in q8_tile.  The gradients
 // go to the entries' places, or by slot into `result` (LDS).  Rows wider than 16 G columns (G = 64) take several sweeps.
@@ -563,15 +571,15 @@ template <int G, int TEAM, bool WIDE>
 __device__ __forceinline__ void q8_dots(const Q8Args& a, RowSampler& s, int t, int count, int most, int32_t base, int32_t spare,
                                         int64_t r, uint32_t* tile, float (&dy)[kQ8Cols], float f, float* result)
 {
-    constexpr int U = G < 4 ? G : 4;
-    const int l = t & (G - 1), e = t / G;
+    constexpr int U = G < 4 ? G : 4, E = TEAM / G;
+    const int l = t & (G - 1), e = t / G, first = q8_slot<G, TEAM>(t);
     int64_t p[4];
     int32_t c[4];
     float w[4], d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int m = 0; m < 4; ++m) {
         const uint32_t entry = s.next();
-        p[m] = t + m * TEAM < count ? (int64_t)base + entry : (int64_t)spare;
+        p[m] = first + m * TEAM < count ? (int64_t)base + entry : (int64_t)spare;
         c[m] = a.colidx[p[m]];
     }
 #pragma unroll
@@ -589,7 +597,7 @@ __device__ __forceinline__ void q8_dots(const Q8Args& a, RowSampler& s, int t, i
             if (m * TEAM >= most) break;                       // wave-uniform
 #pragma unroll 1
             for (int u0 = 0; u0 < G; u0 += U) {
-                if (TEAM == G && m * TEAM + u0 >= most) break;
+                if (m * TEAM + u0 * E >= most) break;
                 uint4_v q[U];
 #pragma unroll
                 for (int u = 0; u < U; ++u) q[u] = q8_load<WIDE>(a, codes, key[m * TEAM + u0 + u]);
@@ -608,8 +616,8 @@ __device__ __forceinline__ void q8_dots(const Q8Args& a, RowSampler& s, int t, i
     }
 #pragma unroll
     for (int m = 0; m < 4; ++m) {
-        if (t + m * TEAM >= count) continue;
-        if (result) result[t + m * TEAM] = d[m] * w[m];
+        if (first + m * TEAM >= count) continue;
+        if (result) result[first + m * TEAM] = d[m] * w[m];
         else a.Y[p[m]] = d[m] * w[m];
     }
     wave_lds_fence();
@@ -685,7 +693,7 @@ template <int G, int TEAM, int KIND, bool WIDE>
 __global__ void __launch_bounds__(kBlockThreads, 4) es_q8_vals_kernel(const Q8Args a)
 {
     constexpr int ROWS = kWaveSize / TEAM, T = 4 * TEAM;
-    constexpr int RESULTS = KIND != Q8_RANDOM ? 1 : TEAM == kWaveSize ? kQ8MostRandom : 4 * TEAM;   // kept entries of a row
+    constexpr int RESULTS = KIND != Q8_RANDOM ? 1 : kQ8MostRandom / ROWS;   // kept entries of a row, at most
     __shared__ uint32_t lds[kWavesPerBlock * kQ8Tile];
     __shared__ float results[kWavesPerBlock * ROWS * RESULTS];
     __shared__ Q8Slots slots[KIND == Q8_RANDOM ? kWavesPerBlock * kWaveSize : 1];
@@ -705,7 +713,7 @@ __global__ void __launch_bounds__(kBlockThreads, 4) es_q8_vals_kernel(const Q8Ar
                 const float f = row_factor(a.norm, w.n, w.k);
                 for (int s0 = wave * kWaveSize; s0 < count; s0 += kBlockThreads) {
                     RowSampler s;
-                    s.init(a.mode, a.seed, w.r, (uint32_t)w.n, (uint32_t)a.W, (uint32_t)(t0 + s0 + lane), kWaveSize);
+                    s.init(a.mode, a.seed, w.r, (uint32_t)w.n, (uint32_t)a.W, (uint32_t)(t0 + s0 + q8_slot<G, kWaveSize>(lane)), kWaveSize);
                     const int m = min(count - s0, kWaveSize);
                     q8_dots<G, kWaveSize, WIDE>(a, s, lane, m, m, w.base, w.base, w.r, lds + wave * kQ8Tile, dy, f, nullptr);
                 }
@@ -733,7 +741,7 @@ __global__ void __launch_bounds__(kBlockThreads, 4) es_q8_vals_kernel(const Q8Ar
         const int most = __builtin_amdgcn_readfirstlane(w.k), spare = __builtin_amdgcn_readfirstlane(w.base);
         if (most == 0) break;                                  // and so are all that follow
         RowSampler s;
-        q8_sampler(s, w, t, TEAM);
+        q8_sampler(s, w, q8_slot<G, TEAM>(t), TEAM);
         if constexpr (G < 64) q8_load_dy(a, r < 0 ? 0 : r, (t & (G - 1)) * kQ8Cols, dy);
         const float f = row_factor(a.norm, w.n, w.k);
         for (int t0 = 0; t0 < most; t0 += T)

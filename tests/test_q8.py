@@ -577,6 +577,32 @@ def test_every_share_of_a_wave(N, avg, long_row, F):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("N,avg,long_row", [(3000, 6, 2900), (9000, 20, 7000), (26_000, 12, 25_000), (120_000, 6, 9000)])
+@pytest.mark.parametrize("F", [16, 41, 250, 300, 520])
+def test_edge_gradient_of_a_random_sample(N, avg, long_row, F):
+    """Every number of lanes that a row of FastRand's takes, at the widths where that changes."""
+    import oracle
+    import torch
+    rowptr, colidx = graph(N, avg, F, long_row)
+    rng = np.random.default_rng(N + F)
+    dY = rng.standard_normal((N, F)).astype(np.float32)
+    codes, scale, q, s, v = filled(rng.standard_normal((N, F)).astype(np.float32))
+    rows = np.repeat(np.arange(N), np.diff(rowptr))
+    want, tol = np.zeros(colidx.size), np.zeros(colidx.size)
+    for lo in range(0, colidx.size, 100_000):
+        e = slice(lo, lo + 100_000)
+        x, g = v[colidx[e]], dY[rows[e]].astype(np.float64)
+        want[e], tol[e] = (x * g).sum(1), (np.abs(x) * np.abs(g)).sum(1) * (F + 6) * U
+    d = dev(rowptr), dev(colidx), dev(dY)
+    for W, seed in ((1, 0), (5, 2), (64, 9), (65, 9), (127, 0), (128, 3), (224, 9), (225, 9), (256, 0), (257, 1), (384, 9), (385, 9), (1024, 9)):
+        pos, cnt = oracle.kept(rowptr, W, "fastrand", seed)
+        keep = np.zeros(colidx.size, bool)
+        keep[pos[np.arange(pos.shape[1])[None, :] < cnt[:, None]]] = True
+        da = es.es_spmm_q8_backward_vals(*d, codes, scale, torch.full((colidx.size,), float("nan"), device="cuda:0"), W, "fastrand", seed)
+        near(da.cpu().numpy(), want * keep, tol * keep, f"W={W}")
+
+
+@pytest.mark.gpu
 def test_edge_gradient_against_differences():
     """The product is linear in the values, so a central difference of L = <dY, Y> has no truncation error, only the
     product's own rounding: two evaluations, each off by at most its tolerance, over a step of 2 h."""
