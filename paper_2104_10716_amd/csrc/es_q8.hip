@@ -52,6 +52,17 @@ bool grid_of(int64_t items, int64_t per_block, uint32_t* out)
 #define ES_TEAMS(X) X(4, 1, 4) X(8, 1, 4) X(16, 1, 4) X(32, 1, 4) X(16, 3, 2) X(64, 1, 4) X(16, 5, 1) X(32, 3, 2) X(64, 2, 2) \
     X(32, 5, 1) X(64, 3, 1) X(64, 4, 1)
 
+// The lanes that launch_write gives a row.
+template <class T>
+int write_team(int32_t F)
+{
+    const int64_t loads = ((int64_t)F + 15) / 16 * (16 / Dense<T>::V);
+#define ES_TEAM(TEAM_, K_, UR_) if (loads <= (TEAM_) * (K_)) return TEAM_;
+    ES_TEAMS(ES_TEAM)
+#undef ES_TEAM
+    return kWaveSize;
+}
+
 template <class T, int MAP>
 int launch_write(const Q8Write& a, hipStream_t st)
 {
@@ -92,7 +103,7 @@ template <class T>
 int run_write(Q8Write a, hipStream_t st)
 {
     if (!a.rows) return launch_write<T, Q8_ALL>(a, st);
-    if (a.n <= kQ8Scan) return launch_write<T, Q8_SCANNED>(a, st);
+    if (a.n <= kQ8Scan * write_team<T>(a.F)) return launch_write<T, Q8_SCANNED>(a, st);
     const size_t row_bytes = (size_t)a.ldx * sizeof(T);
     const int64_t total = a.n;
     for (int64_t done = 0; done < total; done += kQ8Claims) {  // in order: a later piece's rows replace an earlier one's

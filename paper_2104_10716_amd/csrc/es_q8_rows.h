@@ -105,27 +105,50 @@ struct Q8Write {
 
 // Rows whose index among a call's ids is at most this can be marked in the place of their scale (see below).
 constexpr int64_t kQ8Claims = (1 << 23) - 2;
-constexpr int64_t kQ8Scan = 2048;
+// Up to so many ids per lane of a team the ids are scanned: one launch instead of three, whose time grows with their number.  Random
+// ids, us scanned / marked: F = 8 fp32 (4 lanes), 64 ids 4.4 / 7.4, 256 7.8 / 7.6, 1024 17.5 / 8.2; F = 64 (16 lanes), 1024 7.0 / 8.1, 2048
+// 10.7 / 8.1; F = 128 bf16 (16 lanes), 512 8.3 / 10.3, 1024 12.5 / 10.3; F = 602 fp32 (32 lanes), 2048 5.8 / 7.2.
+constexpr int64_t kQ8Scan = 50;
 
-// Which table row element i of the call goes to, or -1.  Of equal ids the last one is written:
-// Q8_SCANNED looks through the ids behind i; Q8_CLAIMED finds i + 1 in place of the row's scale
+// Which table rows the elements i0 .. i0 + UR - 1 of the call go to, or -1.  Of equal ids the last one is written:
+// Q8_SCANNED looks through the ids behind each; Q8_CLAIMED finds i + 1 in place of the row's scale
 // (es_q8_claim_kernel).  A scale is 0, NaN or at least 2^-126, none of which has the bits of such a mark, so a
 // reader that comes after the row's writer is not misled.  The whole team agrees.
-template <int MAP, int TEAM>
-__device__ __forceinline__ int64_t q8_target(const Q8Write& a, int64_t i, int t)
+template <int MAP, int TEAM, int UR>
+__device__ __forceinline__ void q8_targets(const Q8Write& a, int64_t i0, int t, int64_t (&row)[UR])
 {
-    if (MAP == Q8_ALL) return i;
-    const int32_t row = a.rows[i];
-    if (row < 0 || row >= a.N) return -1;
-    if (MAP == Q8_CLAIMED) {
-        const uint32_t mark = __hip_atomic_load(reinterpret_cast<const uint32_t*>(a.scale) + row, __ATOMIC_RELAXED,
-                                                __HIP_MEMORY_SCOPE_AGENT);
-        return mark == (uint32_t)(i + 1) ? row : -1;
+    int32_t id[UR];
+    uint32_t later[UR];
+#pragma unroll
+    for (int u = 0; u < UR; ++u) {
+        row[u] = i0 + u < a.n ? i0 + u : -1;
+        if (MAP == Q8_ALL) continue;
+        id[u] = i0 + u < a.n ? a.rows[i0 + u] : -1;
+        if (id[u] < 0 || id[u] >= a.N) id[u] = -1;
+        row[u] = id[u];
+        later[u] = 0;
     }
-    uint32_t later = 0;
-    for (int64_t j = i + 1 + t; j < a.n; j += TEAM) later |= a.rows[j] == row;
-    later = team_reduce<TEAM>(later, [](uint32_t x, uint32_t y) { return x | y; });
-    return later ? -1 : row;
+    if constexpr (MAP == Q8_CLAIMED) {
+#pragma unroll
+        for (int u = 0; u < UR; ++u) {
+            if (id[u] < 0) continue;
+            const uint32_t mark = __hip_atomic_load(reinterpret_cast<const uint32_t*>(a.scale) + id[u], __ATOMIC_RELAXED,
+                                                    __HIP_MEMORY_SCOPE_AGENT);
+            if (mark != (uint32_t)(i0 + u + 1)) row[u] = -1;
+        }
+    }
+    if constexpr (MAP == Q8_SCANNED) {
+        const int n = (int)a.n, at = (int)min(i0, a.n);        // both small
+#pragma unroll 4
+        for (int j = at + 1 + t; j < n; j += TEAM) {
+            const int32_t other = a.rows[j];
+#pragma unroll
+            for (int u = 0; u < UR; ++u) later[u] |= j > at + u && other == id[u];
+        }
+#pragma unroll
+        for (int u = 0; u < UR; ++u)
+            if (team_reduce<TEAM>(later[u], [](uint32_t x, uint32_t y) { return x | y; })) row[u] = -1;
+    }
 }
 
 // A team of TEAM lanes holds UR rows in registers, K loads of each per lane.  More rows at a time keep more bytes in flight; the
@@ -148,8 +171,7 @@ __global__ void __launch_bounds__(kBlockThreads) es_q8_write_kernel(const Q8Writ
             Dense<T>::load(x + c, a.F - c, v[u][k]);
         }
     }
-#pragma unroll
-    for (int u = 0; u < UR; ++u) row[u] = i0 + u < a.n ? q8_target<MAP, TEAM>(a, i0 + u, t) : -1;
+    q8_targets<MAP, TEAM>(a, i0, t, row);
 #pragma unroll
     for (int u = 0; u < UR; ++u) {
         uint32_t bits = 0;
@@ -181,7 +203,9 @@ __global__ void __launch_bounds__(kBlockThreads) es_q8_write_wide_kernel(const Q
     __shared__ uint32_t part[kWavesPerBlock];
     const int64_t i = blockIdx.x;
     const int lane = threadIdx.x & (kWaveSize - 1), wave = threadIdx.x >> 6;
-    const int64_t row = q8_target<MAP, kWaveSize>(a, i, lane);
+    int64_t rows[1];
+    q8_targets<MAP, kWaveSize>(a, i, lane, rows);
+    const int64_t row = rows[0];
     // every wave has to know before one of them replaces the mark
     __syncthreads();
     if (row < 0) return;

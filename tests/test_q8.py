@@ -315,6 +315,27 @@ def test_write_at_ids(n, F):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("kind,F", [("fp32", 3), ("fp32", 32), ("fp32", 64), ("fp32", 128), ("fp32", 256), ("bf16", 20), ("fp16", 130), ("bf16", 602)])
+def test_write_at_ids_where_the_way_to_tell_equal_ones_changes(kind, F):
+    import torch
+    rng = np.random.default_rng(F)
+    N = 900
+    whole = dev(rng.standard_normal((3201, F)).astype(np.float32)).to(torch_type(kind))
+    q, s, _ = quantise(whole.float().cpu().numpy())
+    for n in (199, 200, 201, 400, 401, 800, 801, 1600, 1601, 3200, 3201):
+        for ids in (rng.integers(-3, N + 3, n), rng.integers(0, 10, n)):
+            ids = ids.astype(np.int32)
+            codes, scale = table(N, F)
+            want_q, want_s = codes.cpu().numpy(), scale.cpu().numpy()
+            es.es_q8_write(whole[:n], codes, scale, rows=dev(ids))
+            for i, r in enumerate(ids):
+                if 0 <= r < N:
+                    want_q[r, :F], want_q[r, F:], want_s[r] = q[i], 0, s[i]
+            np.testing.assert_array_equal(scale.cpu().numpy(), want_s)
+            np.testing.assert_array_equal(codes.cpu().numpy(), want_q)
+
+
+@pytest.mark.gpu
 def test_more_ids_than_marks():
     """More rows than one pass can tell apart: later pieces replace earlier ones."""
     import torch
