@@ -510,7 +510,7 @@ int es_spmm_q8(const int32_t* rowptr, const int32_t* colidx, const float* vals,
  * es_spmm_backward's and does not read it.)
  *     dvals[p] = f_r * scale[c] * sum over columns of dY[r, :] * code[c, :]
  * for the entries p = (r, c) that W, mode and seed keep, 0 for the others.
- *   dY      N rows of F fp32, row stride ldy >= F (input)
+ *   dY      N rows of F fp32, row stride ldy >= F (input); F up to 2^30 (ES_ERR_UNSUPPORTED)
  *   dvals   [nnz] fp32, entries rowptr[0] to rowptr[N] - 1 written
  *   nnz     rowptr[N], a launch-shape hint; 0: no entries, nothing is written
  * Sums are fp32 in a fixed order.

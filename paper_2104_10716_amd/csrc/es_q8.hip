@@ -12,6 +12,7 @@
 namespace {
 
 constexpr int32_t kMaxF = INT32_MAX - 15;
+constexpr int32_t kMaxValsF = 1 << 30;                         // es_q8_vals_kernel counts columns in 32 bits, past the last one
 constexpr int kComputeUnits = 256;
 
 int element_bytes(int32_t type) { return type == ES_FP32 ? 4 : type == ES_FP16 || type == ES_BF16 ? 2 : 0; }
@@ -409,7 +410,7 @@ int es_spmm_q8_backward_vals(const int32_t* rowptr, const int32_t* colidx, const
     a.row_units = wide ? 0u : (uint32_t)(ldq / kQ8Cols);
     const Q8Plan p = plan_vals(N, nnz, F, W, mode);
     a.piece = p.piece; a.long_k = p.long_k; a.wave_rows = p.wave_rows;
-    if (p.grid_x > INT32_MAX) return ES_ERR_UNSUPPORTED;
+    if (p.grid_x > INT32_MAX || F > kMaxValsF) return ES_ERR_UNSUPPORTED;
     a.nblocks = (uint32_t)p.nblocks; a.blocks_per_xcd = (uint32_t)p.per_xcd; a.long_blocks = (uint32_t)p.long_blocks;
     return wide ? launch_vals<true>(a, p, static_cast<hipStream_t>(stream)) : launch_vals<false>(a, p, static_cast<hipStream_t>(stream));
 }
@@ -463,7 +464,7 @@ int es_q8_weight_grad(const int8_t* codes, int32_t ldq, const float* scale, cons
     if (!dW || misaligned(dW, 4) || misaligned(workspace, 16)) return ES_ERR_INVALID_ARG;
     if (N > 0 && (!G || misaligned(G, 4) || bad_table(codes, scale))) return ES_ERR_INVALID_ARG;
     const GradPlan p = plan_grad(N, F, H, workspace ? workspace_bytes : 0);
-    if (ldq >= 1 << 27 || ldg >= 1 << 27) return ES_ERR_UNSUPPORTED;  // a lane's offset inside 8 rows is held in 32 bits
+    if (ldq >= 1 << 27 || ldg >= 1 << 26) return ES_ERR_UNSUPPORTED;  // a lane's byte offset inside 9 rows is held in 32 bits
     const int64_t grid = (p.parts < kNumXcd ? p.parts : (p.parts + kNumXcd - 1) / kNumXcd * kNumXcd) * p.tiles;
     if (grid > INT32_MAX) return ES_ERR_UNSUPPORTED;
     const bool join = p.parts > 1;

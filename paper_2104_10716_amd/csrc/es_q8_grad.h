@@ -10,6 +10,10 @@
 // side by side.  No data has to be turned for that: a lane loads the same 4 columns of codes (2 of G) of 8 rows, and
 // registers number c of those loads are what the lane owes the c-th of 4 (2) tiles; which 32 columns
 // a tile then has, every fourth (second), is of no consequence until the result is stored.  A narrow dW takes fewer tiles.
+//
+// 233 k rows, 602 x 256: 250 us and 9 us of join, 0.86 PFLOP/s of the three products, bound by the matrix cores at the clock that
+// they hold under load (neither without its conversions nor with operands shared through LDS was the kernel faster); 2.45 M rows,
+// 128 x 128: 280 us and 4 us, bound by HBM (5.2 TB/s).
 #ifndef ES_SPMM_Q8_GRAD_H
 #define ES_SPMM_Q8_GRAD_H
 

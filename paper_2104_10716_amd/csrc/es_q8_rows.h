@@ -3,7 +3,8 @@
 //   scale = fp32(max|x| / 127),  code_c = x_c / scale to the nearest integer, ties to even
 //
 // Both directions move each byte once and are bound by memory: a write reads F elements and writes F16 + 4
-// bytes per row (F16: F rounded up to 16), a read the reverse.
+// bytes per row (F16: F rounded up to 16), a read the reverse: 2.45 M fp32 rows of 128, write 304 us (5.3 TB/s), read 250 us
+// (6.3 TB/s); 16 k bf16 rows of 602 at random ids, write 13 us beside 6 us of marks, 64 k read 22 us (5.4 TB/s).
 #ifndef ES_SPMM_Q8_ROWS_H
 #define ES_SPMM_Q8_ROWS_H
 

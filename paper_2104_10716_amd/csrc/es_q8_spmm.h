@@ -354,8 +354,12 @@ __device__ __forceinline__ void q8_team_sum(float (&acc)[kQ8Cols])
 // The product.  The leading workgroups take the long rows, whose waves would run long after the rest of the
 // launch: 16 of them share those among 1024 rows.  The rest take wave_rows rows per wave, each XCD a contiguous range of
 // rows: TEAM lanes to a row, 64 / TEAM rows side by side, TEAM / G entries of each at once.  TEAM is G, or 4, so that
-// there is nothing, or little, to sum across lanes; or a whole wave, where rows are too few to fill the chip and
-// what counts is how soon the longest is done.
+// there is nothing, or little, to sum across lanes; or half a wave or a whole one, where rows are too few to fill the chip
+// or long, and what counts is how soon the longest is done.
+// An entry costs two requests to the L2, one line of codes and one of scales, or more where rows straddle lines, and a CU keeps
+// some 100 of them in flight: that bounds the product (233 k rows, Bucket of 64, F = 64: 29.5 M requests of 386 clocks in 180 us, 1.0 GB
+// behind the L2s; 2.45 M rows, FastRand of 64, F = 128: 120 M of 563 in 1300 us, 7.0 TB/s behind them; 170 k rows of mean 14, exact,
+// F = 100: 6.7 M of 511 in 92 us).
 // LONG: there may be long rows (a kernel of its own without them keeps its registers).
 template <int G, int TEAM, bool LONG, bool WIDE>
 __global__ void __launch_bounds__(kBlockThreads, 5) es_q8_spmm_kernel(const Q8Args a)
@@ -490,9 +494,11 @@ __global__ void __launch_bounds__(kBlockThreads) es_q8_join_kernel(const Q8Args 
     }
 }
 
-// A few asked rows: every one is cut into up to a.splits equal pieces of 128 slots and more, a workgroup each.
+// A few asked rows: every one is cut into up to a.splits equal pieces of 128 slots and more, a workgroup each.  Latency bounds
+// it: 32 rows of mean 490, F = 64: 4.3 us, and 2.8 us to join the pieces.
 __device__ __forceinline__ int32_t q8_few_length(const Q8Args& a, int32_t k)
 {
+    if (a.splits == 1) return k;
     const int32_t each = (k - 1) / a.splits + 1;
     return each <= 128 ? 128 : (each + 63) & ~63;
 }
@@ -683,7 +689,9 @@ constexpr int32_t kQ8MostRandom = 1024;                        // largest W whos
 
 enum { Q8_PREFIX = 0, Q8_LONG = 1, Q8_RANDOM = 2 };
 
-// Rows and waves as in es_q8_spmm_kernel.  What is not kept gets its zeros in the same pass:
+// Rows and waves as in es_q8_spmm_kernel, and the same bound, next to reading dY and writing dvals (170 k rows of mean 14, Bucket of 16,
+// F = 128: 39 us, 5.8 TB/s; 233 k of mean 490, FastRand of 64, F = 41: 393 us, 36.9 M requests).  What is not kept gets its zeros in
+// the same pass:
 //  * Q8_PREFIX: all of a row is kept, or its first entries (full, Bucket); the wave clears what is behind them
 //  * Q8_LONG: the same where there may be long rows; here and in Q8_PREFIX FastRand's zeros are there before (es_q8_zero_kernel)
 //  * Q8_RANDOM: the kept entries lie anywhere in the row.  Zeros and gradients written one after the other would be two

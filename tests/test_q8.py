@@ -142,6 +142,14 @@ def test_refusals_answer_on_the_host():
     assert ask(100, 16, 16) == 0 and ask(1_000_000, 128, 128) > 0
 
 
+def test_widths_beyond_the_kernels_offsets_are_refused():
+    lib = es.load_library()
+    F = 2 ** 30 + 1
+    assert lib.es_spmm_q8_backward_vals(FAKE, FAKE, FAKE, F, FAKE, F + 15, FAKE, FAKE, 4, 9, F, 2, 1, 0, 0, None) == -2
+    for ldq, ldg, H in ((32, 2 ** 26, 8), (32, 2 ** 27 - 1, 2 ** 27 - 1), (2 ** 27, 8, 8)):
+        assert lib.es_q8_weight_grad(FAKE, ldq, FAKE, FAKE, ldg, FAKE, H, 100, 20, H, None, 0, None) == -2
+
+
 def test_python_refuses_what_it_cannot_read():
     import torch
     from torch._subclasses.fake_tensor import FakeTensorMode
