@@ -440,6 +440,9 @@ int es_spmm_launch_info(int64_t N, int64_t nnz, int32_t F, int32_t ldx, int32_t 
  *   codes  [N x ldq] int8 (device), 16-byte aligned, ldq a multiple of 16 and >= F;
  *          es_q8_row_bytes(F) is the smallest, F rounded up to 16.  Columns F to
  *          es_q8_row_bytes(F) - 1 are written as 0; readers ignore them.  N < 2^31.
+ *          Rows that tile no 128-byte line cost the products more lines: with ldq = 128
+ *          instead of 112 the exact product of F = 100 takes 0.64 to 0.84 of the time
+ *          (170 k to 2.45 M rows); F of 16, 32 and 64 and small tables gain nothing.
  *   scale  [N] fp32 (device)
  * Dense matrices beside the table may have any row stride >= their width and any
  * alignment of their elements' size.

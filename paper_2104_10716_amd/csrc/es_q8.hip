@@ -214,8 +214,9 @@ Q8Plan plan_q8(int64_t N, int64_t nnz, int32_t F, int32_t W, int32_t mode, int64
     Q8Plan p = {};
     const int64_t chunks = ((int64_t)F + 15) / 16;
     p.G = chunks >= 16 ? 16 : next_pow2(chunks);
-    // Wider rows go in blocks of 256 columns, each of which gathers the entries' scales and values anew.  Blocks of 128: 128 k
-    // rows of mean 50, F = 144 / 256 / 272 / 602: 366 / 310 / 513 / 870 us, of 256: 239 / 233 / 432 / 693.
+    // Wider rows go in blocks of 256 columns, each of which gathers the entries' scales and values anew.  Blocks of 128, 128 k
+    // rows of mean 50, F = 256 / 272 / 602: 310 / 513 / 870 us, of 256: 233 / 432 / 693.  The last block's columns as a launch of its
+    // own with fewer lanes: 0.92 to 1.05 of the time from 60 k rows on (F = 272 to 1072), 1.0 to 1.4 below.
     p.slices = (chunks + p.G - 1) / p.G;
     const int64_t Wk = mode == ES_FULL ? INT32_MAX : W;
     double mean = N > 0 ? (double)nnz / (double)N : 0.0;

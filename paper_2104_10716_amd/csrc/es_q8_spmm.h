@@ -375,7 +375,7 @@ __global__ void __launch_bounds__(kBlockThreads, 5) es_q8_spmm_kernel(const Q8Ar
     const int lane = threadIdx.x & (kWaveSize - 1), wave = threadIdx.x >> 6;
     const int l = lane & (G - 1);
     const int c0 = (blockIdx.y * G + l) * kQ8Cols;
-    const int8_t* codes = a.codes + (c0 < a.F ? c0 : 0);       // lanes behind the last column load the first ones
+    const int8_t* codes = a.codes + min(c0, (a.F - 1) & -kQ8Cols);   // lanes behind the last columns load those: no line of their own
     float acc[kQ8Cols];
 
     if constexpr (LONG) {
@@ -510,7 +510,7 @@ __global__ void __launch_bounds__(kBlockThreads) es_q8_few_kernel(const Q8Args a
     __shared__ uint2 lds[kQ8Lds];
     const int lane = threadIdx.x & (kWaveSize - 1), wave = threadIdx.x >> 6;
     const int c0 = (blockIdx.y * G + (lane & (G - 1))) * kQ8Cols;
-    const int8_t* codes = a.codes + (c0 < a.F ? c0 : 0);
+    const int8_t* codes = a.codes + min(c0, (a.F - 1) & -kQ8Cols);
     const int64_t i = blockIdx.x % a.n_rows;                   // pieces of one row go to different XCDs' queues last
     const int piece = (int)(blockIdx.x / a.n_rows);
     const Q8Row w = q8_row(a, i);
@@ -597,7 +597,7 @@ __device__ __forceinline__ void q8_dots(const Q8Args& a, RowSampler& s, int t, i
     const uint32_t* key = tile + e * G;
     for (int c0 = l * kQ8Cols; c0 - l * kQ8Cols < a.F; c0 += G * kQ8Cols) {
         if constexpr (G == 64) q8_load_dy(a, r < 0 ? 0 : r, c0, dy);
-        const int8_t* codes = a.codes + (c0 < a.F ? c0 : 0);
+        const int8_t* codes = a.codes + min(c0, (a.F - 1) & -kQ8Cols);
 #pragma unroll
         for (int m = 0; m < 4; ++m) {
             if (m * TEAM >= most) break;                       // wave-uniform
