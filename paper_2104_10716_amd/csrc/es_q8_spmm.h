@@ -475,22 +475,25 @@ __global__ void __launch_bounds__(kBlockThreads) es_q8_join_kernel(const Q8Args 
     const int64_t first = (int64_t)blockIdx.x * kQ8ScanRows;
     if (threadIdx.x == 0) found = 0;
     __syncthreads();
-    for (int m = threadIdx.x; m < kQ8ScanRows; m += kBlockThreads)
-        if (q8_row(a, first + m).k > a.piece) any[atomicAdd(&found, 1)] = m;   // their order is of no consequence
+    int32_t k[kQ8ScanRows / kBlockThreads];
+#pragma unroll
+    for (int m = 0; m < kQ8ScanRows / kBlockThreads; ++m) k[m] = q8_row(a, first + m * kBlockThreads + threadIdx.x).k;
+#pragma unroll
+    for (int m = 0; m < kQ8ScanRows / kBlockThreads; ++m)
+        if (k[m] > a.piece) any[atomicAdd(&found, 1)] = m * kBlockThreads + threadIdx.x;   // their order is of no consequence
     __syncthreads();
-    for (int x = 0; x < found; ++x) {
-        const int64_t i = first + any[x];
+    // a wave takes 64 columns of a row
+    const int64_t groups = ((int64_t)a.F + kWaveSize - 1) / kWaveSize;
+    for (int64_t task = threadIdx.x / kWaveSize; task < found * groups; task += kWavesPerBlock) {
+        const int64_t i = first + any[task / groups], c = task % groups * kWaveSize + (threadIdx.x & (kWaveSize - 1));
         const Q8Row w = q8_row(a, i);
-        const float f = row_factor(a.norm, w.n, w.k);
         const int64_t span = w.base / a.piece;
-        const int pieces = q8_pieces(a, w);
-        for (int c = threadIdx.x; c < a.F; c += kBlockThreads) {
-            const float s = q8_sum_pieces(pieces, [&](int p) {
-                const int64_t at = 2 * (span + p) + (p == 0 ? 1 : 0);
-                return at < a.pieces ? a.partial[at * a.F + c] : 0.0f;
-            });
-            a.Y[i * (int64_t)a.ldy + c] = s * f;
-        }
+        if (c >= a.F) continue;
+        const float s = q8_sum_pieces(q8_pieces(a, w), [&](int p) {
+            const int64_t at = 2 * (span + p) + (p == 0 ? 1 : 0);
+            return at < a.pieces ? a.partial[at * a.F + c] : 0.0f;
+        });
+        a.Y[i * (int64_t)a.ldy + c] = s * row_factor(a.norm, w.n, w.k);
     }
 }
 
