@@ -194,7 +194,12 @@ void plan_rows(Q8Plan& p, int64_t n_rows, double mean, int64_t Wk)
     // F = 96, mean 4.6 468 / 455; the edge gradient, 544 k, F = 102, mean 41 533 / 549, 1.2 M, F = 48, mean 16 551 / 522.
     const int side = kWaveSize / p.team;                       // rows side by side
     p.wave_rows = mean >= 24.0 ? 32 : 64;
-    while (p.wave_rows > side && n_rows / p.wave_rows < 8 * 4 * kComputeUnits) p.wave_rows /= 2;
+    // Where one row or two run at a time, their order counts for less than even ends, 32 waves per SIMD instead of 8: 233 k rows, Bucket 64, F = 64
+    // 180 / 171 us; the edge gradient, 224 k, Bucket 27, F = 344 303 / 278, 233 k, FastRand 500, F = 400 567 / 536.  Two rows of FastRand's edge
+    // gradient, whose last pass takes them in turn, 60 k, W = 100, F = 100 47.5 / 51.7; eight of 170 k, mean 14 102 / 106.  It costs one row of
+    // the edge gradient's at F = 128, FastRand of 250, 60 k rows: 90 / 99.
+    const int64_t waves = (side == 1 || (side == 2 && !p.random) ? 32 : 8) * 4 * kComputeUnits;
+    while (p.wave_rows > side && n_rows / p.wave_rows < waves) p.wave_rows /= 2;
     // a lane retires a batch of entries in some 1.5 us; a row should not take it a tenth of the launch
     const double us = mean * (double)n_rows * (double)(p.slices * (p.G * 16 + 12)) / 5.0e6;
     const double side_by_side = (double)p.team / (double)p.G;  // entries of a row

@@ -357,7 +357,7 @@ __device__ __forceinline__ void q8_team_sum(float (&acc)[kQ8Cols])
 // there is nothing, or little, to sum across lanes; or half a wave or a whole one, where rows are too few to fill the chip
 // or long, and what counts is how soon the longest is done.
 // An entry costs two requests to the L2, one line of codes and one of scales, or more where rows straddle lines, and a CU keeps
-// some 100 of them in flight: that bounds the product (233 k rows, Bucket of 64, F = 64: 29.5 M requests of 386 clocks in 180 us, 1.0 GB
+// some 100 of them in flight: that bounds the product (233 k rows, Bucket of 64, F = 64: 29.6 M requests of 384 clocks in 171 us, 1.0 GB
 // behind the L2s; 2.45 M rows, FastRand of 64, F = 128: 120 M of 563 in 1300 us, 7.0 TB/s behind them; 170 k rows of mean 14, exact,
 // F = 100: 6.7 M of 511 in 92 us).
 // LONG: there may be long rows (a kernel of its own without them keeps its registers).
