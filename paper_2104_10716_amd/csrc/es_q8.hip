@@ -242,8 +242,10 @@ Q8Plan plan_q8(int64_t N, int64_t nnz, int32_t F, int32_t W, int32_t mode, int64
     }
     p.team = pick_team(p.G, n_rows, mean);
     plan_rows(p, n_rows, mean, Wk);
+    // The join sums every row that keeps more than `piece`, so all of those have to be long ones, which workgroups cut: a wave stores
+    // a row of up to long_k by itself.
     int64_t piece = 1024;
-    while (piece * 8192 < nnz) piece *= 2;
+    while (piece * 8192 < nnz || piece < p.long_k) piece *= 2;
     p.pieces = Wk > piece && nnz > piece ? 2 * (nnz / piece + 1) : 0;
     p.piece = p.pieces ? (int32_t)piece : INT32_MAX;
     return p;

@@ -36,7 +36,7 @@ struct Q8Args {
     int32_t F, ldq, ldy, W, mode, norm;
     uint32_t row_units;        // ldq / 16: the row stride of the codes in lane loads
     int32_t long_k;            // rows keeping more entries are a workgroup's, not a wave's
-    int32_t piece;             // and those keeping more than this are cut into pieces
+    int32_t piece;             // and those keeping more than this are cut into pieces (the product's is at least long_k)
     int64_t pieces;            // capacity of `partial`
     uint32_t nblocks, blocks_per_xcd, long_blocks;
     int32_t splits;            // es_q8_few_kernel: pieces a row may be cut into
@@ -467,7 +467,7 @@ __device__ __forceinline__ float q8_sum_pieces(int pieces, Get&& get)
     return s;
 }
 
-// Rows that were cut: the sum of their pieces in order, times the factor.
+// Rows that were cut, which are all that keep more than `piece` entries: the sum of their pieces in order, times the factor.
 __global__ void __launch_bounds__(kBlockThreads) es_q8_join_kernel(const Q8Args a)
 {
     __shared__ int any[kQ8ScanRows];
