@@ -198,10 +198,11 @@ __device__ __forceinline__ void q8_block_sum(const Q8Args& a, const Q8Row& w, in
     for (int j = 0; j < kQ8Cols; ++j) acc[j] = 0.0f;
     // short pieces are dealt in smaller shares, so that all four waves have some
     const int step = count >= kWavesPerBlock * kQ8Tile ? kQ8Tile : max(E * kQ8Batch, 64);
-    for (int32_t s = wave * step; s < count; s += kWavesPerBlock * step) {
+    // slots unsigned: the one behind the last may be beyond 2^31
+    for (uint32_t s = wave * step; s < (uint32_t)count; s += kWavesPerBlock * step) {
         RowSampler sampler;
-        sampler.init(a.mode, a.seed, w.r, (uint32_t)w.n, (uint32_t)a.W, (uint32_t)(t0 + s + lane), kWaveSize);
-        const int m = min(count - s, step);
+        sampler.init(a.mode, a.seed, w.r, (uint32_t)w.n, (uint32_t)a.W, (uint32_t)t0 + s + lane, kWaveSize);
+        const int m = (int)min((uint32_t)count - s, (uint32_t)step);
         q8_tile<G, kWaveSize, WIDE>(a, sampler, lane, m, m, w.base, w.base, tile, codes, acc);
     }
     Sum::run(acc);

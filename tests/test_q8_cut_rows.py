@@ -162,3 +162,35 @@ def test_wide_rows_whose_time_moves_the_border():
         c = graph[1][e].long()
         x = codes[c].double() * scale[c].double()[:, None] * graph[2][e].double()[:, None]
         near(Y[r].cpu().numpy(), x.sum(0).cpu().numpy(), x.abs().sum(0).cpu().numpy() * (deg[r] + 5) * U, f"row {r} of {deg[r]}")
+
+
+@pytest.mark.gpu
+def test_a_row_of_all_entries_that_there_can_be():
+    """2^31 - 1 entries, all of one row: counts past the last one do not fit 31 bits.  Every entry but a handful names a row
+    of zeros, so the sums are exact."""
+    import torch
+    n, F = 2 ** 31 - 1, 16
+    colidx = torch.zeros(n, dtype=torch.int32, device="cuda:0")            # 8.6 GB
+    named = [0, 1023, 2 ** 30, n - 1025, n - 1024, n - 2, n - 1]
+    colidx[torch.tensor(named, device="cuda:0")] = 1
+    rowptr = torch.tensor([0, 0, n], dtype=torch.int32, device="cuda:0")
+    codes = torch.tensor([[0] * F, list(range(-8, 8))], dtype=torch.int8, device="cuda:0")
+    scale = torch.tensor([1.0, 0.5], device="cuda:0")
+    want = codes[1].float() * (0.5 * len(named))
+    none = torch.empty(0, dtype=torch.uint8, device="cuda:0")
+    # one workgroup takes the row; 64 share it; every entry but one, in another order
+    for mode, W, workspace in (("full", 0, none), ("full", 0, None), ("fastrand", n - 1, None)):
+        Y = torch.full((2, F), float("nan"), device="cuda:0")
+        es.es_spmm_q8(rowptr, colidx, None, codes, scale, Y, W, mode, workspace=workspace)
+        torch.cuda.synchronize()
+        assert bool((Y[0] == 0).all()) and torch.equal(Y[1], want), (mode, Y)
+    dY = torch.ones((2, F), device="cuda:0")
+    dvals = torch.full((n,), 7.0, device="cuda:0")
+    each = float(codes[1].float().sum() * 0.5)
+    for mode, W in (("full", 0), ("bucket", n - 1), ("fastrand", n - 1)):
+        es.es_spmm_q8_backward_vals(rowptr, colidx, dY, codes, scale, dvals, W, mode)
+        left = {"full": -1, "bucket": n - 1, "fastrand": (n - 1) * 577 % n}[mode]
+        for p in named:
+            assert float(dvals[p]) == (0.0 if p == left else each), (mode, p)
+        assert int(torch.count_nonzero(dvals)) == len(named) - (left in named), mode
+        dvals.fill_(7.0)
