@@ -495,7 +495,8 @@ int es_q8_read(const int8_t* codes, int32_t ldq, const float* scale, int64_t N, 
  *           (same stream).  With a smaller one, or none, such a row is one workgroup's.
  * Accumulation is fp32 in an order that the sizes and the workspace fix: the same
  * call gives the same bits.  A row of the table that no kept entry names has no
- * influence, whatever it holds.
+ * influence, whatever it holds.  ES_ERR_UNSUPPORTED for F above 16 776 960, and where the
+ * rows are more than a launch holds (never up to 700 million).
  */
 size_t es_spmm_q8_workspace_bytes(int64_t N, int64_t nnz, int32_t F, int32_t W, int32_t mode,
                                   int64_t n_rows);
@@ -516,7 +517,8 @@ int es_spmm_q8(const int32_t* rowptr, const int32_t* colidx, const float* vals,
  *   dY      N rows of F fp32, row stride ldy >= F (input); F up to 2^30 (ES_ERR_UNSUPPORTED)
  *   dvals   [nnz] fp32, entries rowptr[0] to rowptr[N] - 1 written
  *   nnz     rowptr[N], a launch-shape hint; 0: no entries, nothing is written
- * Sums are fp32 in a fixed order.
+ * Sums are fp32 in a fixed order.  ES_ERR_UNSUPPORTED where the rows are more than a launch
+ * holds (never up to 700 million).
  */
 int es_spmm_q8_backward_vals(const int32_t* rowptr, const int32_t* colidx,
                              const float* dY, int32_t ldy, const int8_t* codes, int32_t ldq,

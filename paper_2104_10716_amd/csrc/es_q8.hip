@@ -40,13 +40,13 @@ int next_pow2(int64_t v)
 
 int launched() { return hipGetLastError() == hipSuccess ? ES_OK : ES_ERR_LAUNCH; }
 
-bool grid_of(int64_t items, int64_t per_block, uint32_t* out)
-{
-    const int64_t blocks = (items + per_block - 1) / per_block;
-    if (blocks < 1 || blocks > INT32_MAX) return false;
-    *out = (uint32_t)blocks;
-    return true;
-}
+// A launch holds fewer than 2^32 threads along x.
+constexpr int64_t kMostBlocks = UINT32_MAX / kBlockThreads;
+// Rows of a table that one launch writes or reads, a workgroup for each of them at most; longer lists take several.
+constexpr int64_t kLaunchRows = (1 << 24) - 4096;
+static_assert(kLaunchRows <= kMostBlocks && kQ8Claims <= kMostBlocks, "");
+
+uint32_t blocks_of(int64_t items, int64_t per_block) { return (uint32_t)((items + per_block - 1) / per_block); }
 
 // Lanes to a row of so many 16-byte accesses, accesses per lane, and rows at a time: the fewest idle lanes.  233 k rows of 602
 // bf16 with 64 lanes throughout: written in 127 us and read in 100, this way 95 and 93; of 602 fp32: read in 188, 154.
@@ -68,18 +68,16 @@ template <class T, int MAP>
 int launch_write(const Q8Write& a, hipStream_t st)
 {
     const int64_t loads = ((int64_t)a.F + 15) / 16 * (16 / Dense<T>::V);
-    uint32_t grid;
 #define ES_WRITE(TEAM_, K_, UR_)                                                                                            \
     if (loads <= (TEAM_) * (K_)) {                                                                                          \
-        if (!grid_of(a.n, (int64_t)(kBlockThreads / (TEAM_)) * (UR_), &grid)) return ES_ERR_UNSUPPORTED;                    \
+        const uint32_t grid = blocks_of(a.n, (int64_t)(kBlockThreads / (TEAM_)) * (UR_));                                   \
         hipLaunchKernelGGL((es_q8_write_kernel<T, TEAM_, K_, UR_, MAP>), dim3(grid), dim3(kBlockThreads), 0, st, a);        \
         return launched();                                                                                                  \
     }
     ES_TEAMS(ES_WRITE)
     if constexpr (Dense<T>::V == 4) { ES_WRITE(64, 8, 1) }
 #undef ES_WRITE
-    if (!grid_of(a.n, 1, &grid)) return ES_ERR_UNSUPPORTED;
-    hipLaunchKernelGGL((es_q8_write_wide_kernel<T, MAP>), dim3(grid), dim3(kBlockThreads), 0, st, a);
+    hipLaunchKernelGGL((es_q8_write_wide_kernel<T, MAP>), dim3((uint32_t)a.n), dim3(kBlockThreads), 0, st, a);
     return launched();
 }
 
@@ -87,10 +85,9 @@ template <class T>
 int launch_read(const Q8Read& a, hipStream_t st)
 {
     const int64_t stores = ((int64_t)a.F + Dense<T>::V - 1) / Dense<T>::V;
-    uint32_t grid;
 #define ES_READ(TEAM_, K_, UR_)                                                                                             \
     if (stores <= (TEAM_) * (K_) || (TEAM_) * (K_) == 256) {                                                                \
-        if (!grid_of(a.n, (int64_t)(kBlockThreads / (TEAM_)) * (UR_), &grid)) return ES_ERR_UNSUPPORTED;                    \
+        const uint32_t grid = blocks_of(a.n, (int64_t)(kBlockThreads / (TEAM_)) * (UR_));                                   \
         hipLaunchKernelGGL((es_q8_read_kernel<T, TEAM_, K_, UR_>), dim3(grid), dim3(kBlockThreads), 0, st, a);              \
         return launched();                                                                                                  \
     }
@@ -103,22 +100,52 @@ int launch_read(const Q8Read& a, hipStream_t st)
 template <class T>
 int run_write(Q8Write a, hipStream_t st)
 {
-    if (!a.rows) return launch_write<T, Q8_ALL>(a, st);
-    if (a.n <= kQ8Scan * write_team<T>(a.F)) return launch_write<T, Q8_SCANNED>(a, st);
     const size_t row_bytes = (size_t)a.ldx * sizeof(T);
     const int64_t total = a.n;
+    if (!a.rows) {
+        for (int64_t done = 0; done < total; done += kLaunchRows) {
+            Q8Write b = a;
+            b.n = total - done < kLaunchRows ? total - done : kLaunchRows;
+            b.X = static_cast<const char*>(a.X) + (size_t)done * row_bytes;
+            b.codes = a.codes + done * a.ldq;
+            b.scale = a.scale + done;
+            const int rc = launch_write<T, Q8_ALL>(b, st);
+            if (rc != ES_OK) return rc;
+        }
+        return ES_OK;
+    }
+    if (a.n <= kQ8Scan * write_team<T>(a.F)) return launch_write<T, Q8_SCANNED>(a, st);
     for (int64_t done = 0; done < total; done += kQ8Claims) {  // in order: a later piece's rows replace an earlier one's
         Q8Write b = a;
         b.n = total - done < kQ8Claims ? total - done : kQ8Claims;
         b.rows = a.rows + done;
         b.X = static_cast<const char*>(a.X) + (size_t)done * row_bytes;
-        uint32_t grid;
-        if (!grid_of(b.n, kBlockThreads, &grid)) return ES_ERR_UNSUPPORTED;
+        const uint32_t grid = blocks_of(b.n, kBlockThreads);
         hipLaunchKernelGGL(es_q8_claim_kernel<false>, dim3(grid), dim3(kBlockThreads), 0, st, b);
         if (launched() != ES_OK) return ES_ERR_LAUNCH;
         hipLaunchKernelGGL(es_q8_claim_kernel<true>, dim3(grid), dim3(kBlockThreads), 0, st, b);
         if (launched() != ES_OK) return ES_ERR_LAUNCH;
         const int rc = launch_write<T, Q8_CLAIMED>(b, st);
+        if (rc != ES_OK) return rc;
+    }
+    return ES_OK;
+}
+
+template <class T>
+int run_read(const Q8Read& a, hipStream_t st)
+{
+    for (int64_t done = 0; done < a.n; done += kLaunchRows) {
+        Q8Read b = a;
+        b.n = a.n - done < kLaunchRows ? a.n - done : kLaunchRows;
+        b.Y = static_cast<T*>(a.Y) + done * a.ldy;
+        if (a.rows) {
+            b.rows = a.rows + done;
+        } else {
+            b.codes = a.codes + done * a.ldq;
+            b.scale = a.scale + done;
+            b.N = a.N - done;
+        }
+        const int rc = launch_read<T>(b, st);
         if (rc != ES_OK) return rc;
     }
     return ES_OK;
@@ -359,7 +386,7 @@ int es_q8_read(const int8_t* codes, int32_t ldq, const float* scale, int64_t N, 
     if (!Y || misaligned(Y, size) || misaligned(rows, 4) || (N > 0 && bad_table(codes, scale))) return ES_ERR_INVALID_ARG;
     const Q8Read a = {codes, scale, rows, Y, n, N, F, ldq, ldy};
     hipStream_t st = static_cast<hipStream_t>(stream);
-    return type == ES_FP32 ? launch_read<float>(a, st) : type == ES_FP16 ? launch_read<_Float16>(a, st) : launch_read<__bf16>(a, st);
+    return type == ES_FP32 ? run_read<float>(a, st) : type == ES_FP16 ? run_read<_Float16>(a, st) : run_read<__bf16>(a, st);
 }
 
 size_t es_spmm_q8_workspace_bytes(int64_t N, int64_t nnz, int32_t F, int32_t W, int32_t mode, int64_t n_rows)
@@ -396,7 +423,7 @@ int es_spmm_q8(const int32_t* rowptr, const int32_t* colidx, const float* vals, 
     a.row_units = wide ? 0u : (uint32_t)(ldq / kQ8Cols);
     a.partial = static_cast<float*>(workspace);
     a.pieces = p.pieces; a.piece = p.piece; a.long_k = p.long_k; a.splits = p.splits; a.wave_rows = p.wave_rows;
-    if (p.grid_x > INT32_MAX || p.slices > 65535) return ES_ERR_UNSUPPORTED;
+    if (p.grid_x > kMostBlocks || p.slices > 65535) return ES_ERR_UNSUPPORTED;
     a.nblocks = (uint32_t)p.nblocks; a.blocks_per_xcd = (uint32_t)p.per_xcd; a.long_blocks = (uint32_t)p.long_blocks;
     return wide ? launch_q8<true>(a, p, static_cast<hipStream_t>(stream)) : launch_q8<false>(a, p, static_cast<hipStream_t>(stream));
 }
@@ -418,7 +445,7 @@ int es_spmm_q8_backward_vals(const int32_t* rowptr, const int32_t* colidx, const
     a.row_units = wide ? 0u : (uint32_t)(ldq / kQ8Cols);
     const Q8Plan p = plan_vals(N, nnz, F, W, mode);
     a.piece = p.piece; a.long_k = p.long_k; a.wave_rows = p.wave_rows;
-    if (p.grid_x > INT32_MAX || F > kMaxValsF) return ES_ERR_UNSUPPORTED;
+    if (p.grid_x > kMostBlocks || F > kMaxValsF) return ES_ERR_UNSUPPORTED;
     a.nblocks = (uint32_t)p.nblocks; a.blocks_per_xcd = (uint32_t)p.per_xcd; a.long_blocks = (uint32_t)p.long_blocks;
     return wide ? launch_vals<true>(a, p, static_cast<hipStream_t>(stream)) : launch_vals<false>(a, p, static_cast<hipStream_t>(stream));
 }
@@ -474,7 +501,7 @@ int es_q8_weight_grad(const int8_t* codes, int32_t ldq, const float* scale, cons
     const GradPlan p = plan_grad(N, F, H, workspace ? workspace_bytes : 0);
     if (ldq >= 1 << 27 || ldg >= 1 << 26) return ES_ERR_UNSUPPORTED;  // a lane's byte offset inside 9 rows is held in 32 bits
     const int64_t grid = (p.parts < kNumXcd ? p.parts : (p.parts + kNumXcd - 1) / kNumXcd * kNumXcd) * p.tiles;
-    if (grid > INT32_MAX) return ES_ERR_UNSUPPORTED;
+    if (grid > kMostBlocks) return ES_ERR_UNSUPPORTED;
     const bool join = p.parts > 1;
     const Q8Grad a = {codes, scale, G, join ? static_cast<float*>(workspace) : dW, N, F, H, ldq, ldg, join ? H : ldw,
                       (int32_t)p.tiles_m, (int32_t)p.tiles, p.part_rows, (int32_t)p.parts};
@@ -486,8 +513,7 @@ int es_q8_weight_grad(const int8_t* codes, int32_t ldq, const float* scale, cons
 #undef ES_GRAD
     if (launched() != ES_OK) return ES_ERR_LAUNCH;
     if (!join) return ES_OK;
-    uint32_t gj;
-    if (!grid_of((int64_t)F * H, kWaveSize, &gj)) return ES_ERR_UNSUPPORTED;
+    const uint32_t gj = blocks_of((int64_t)F * H, kWaveSize);      // several parts: 256 tiles of dW or fewer
     hipLaunchKernelGGL(es_q8_grad_join_kernel, dim3(gj), dim3(kGradJoin * kWaveSize), 0, st, a.dW, (int)p.parts, F, H, dW, ldw);
     return launched();
 }

@@ -87,3 +87,54 @@ def test_the_asked_workspace_is_the_planned_one(ask):
     queries = list(sweep())[::11]
     for q, p, size in zip(queries, plans(ask, queries), ask([("bytes",) + q for q in queries])):
         assert int(size) == 4 * q[2] * p["pieces"], (q, p)
+
+
+def launches(line, fields):
+    """(status, [(blocks, threads, ...)]) of an answer."""
+    words = list(map(int, line.split()))
+    rest = words[1:]
+    assert len(rest) % fields == 0, line
+    return words[0], [tuple(rest[i:i + fields]) for i in range(0, len(rest), fields)]
+
+
+def test_every_launch_has_fewer_than_2_to_32_threads(ask):
+    """That is what a launch can hold along x.  Beyond it a call is refused before its first launch."""
+    many = (1, 5000, 2_450_000, 2 ** 24, 20_000_000, 70_000_000, 300_000_000, 700_000_000, 900_000_000, 2 ** 31 - 1)
+    queries = []
+    for N in many:
+        for F in (1, 16, 100, 256, 1000, 4000):
+            for nnz in (N // 2 + 1, N, min(3 * N, 2 ** 31 - 1), 2 ** 31 - 1):
+                for W, mode in ((0, FULL), (4, BUCKET), (900, FASTRAND), (5000, FASTRAND)):
+                    queries.append(("vals", N, nnz, F, W, mode))
+                    queries += [("spmm", N, nnz, F, W, mode, n, ws) for n in (1, 512, N) for ws in (0, 1)]
+            queries += [("grad", N, F, H, ws) for H in (1, 100, 5000, 2_000_000) for ws in (0, 1)]
+    queries += [("grad", 100, F, H, 1) for F in (1, 100, 2 ** 26, 2 ** 27 - 16) for H in (1, 2 ** 20, 2 ** 26 - 1)]
+    served = refused = 0
+    for q, line in zip(queries, ask(queries)):
+        status, made = launches(line, 2)
+        assert status in (0, -2), (q, line)
+        assert (status == 0) == (len(made) > 0), (q, line)
+        assert all(0 < blocks * threads < 2 ** 32 for blocks, threads in made), (q, line)
+        if q[1] <= 700_000_000 and q[0] != "grad":
+            assert status == 0, (q, line)
+        served += status == 0
+        refused += status == -2
+    assert served > 1000 and refused > 20
+
+
+def test_long_lists_of_rows_are_written_and_read_in_order(ask):
+    """Whole tables and lists of ids in one launch after the other, none too large, none left out."""
+    queries = [(what, kind, n, F, ids, n) for what in ("write", "read") for kind in (0, 1, 2) for ids in (0, 1)
+               for n in (1, 4000, 2 ** 23 - 2, 2 ** 24 - 1, 2 ** 24, 2 ** 25 + 3, 700_000_000, 2 ** 31 - 1)
+               for F in (1, 16, 64, 100, 128, 300, 600, 700, 1024, 1500, 2048, 2049, 4096, 100_000)]
+    for q, line in zip(queries, ask(queries)):
+        status, made = launches(line, 4)
+        assert status == 0 and made, (q, line)
+        assert all(0 < blocks * threads < 2 ** 32 for blocks, threads, _, _ in made), (q, line)
+        marks = q[0] == "write" and q[4] and len(made) % 3 == 0 and q[2] > 3200
+        pieces = made[2::3] if marks else made
+        done = 0
+        for blocks, threads, rows, first in pieces:
+            assert first == (0 if q[4] else done), (q, line)
+            done += rows
+        assert done == q[2], (q, line)
