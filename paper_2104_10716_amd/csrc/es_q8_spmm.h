@@ -511,7 +511,7 @@ template <int G, bool WIDE>
 __global__ void __launch_bounds__(kBlockThreads) es_q8_few_kernel(const Q8Args a)
 {
     using Sum = Q8Sum<G, kWaveSize>;
-    __shared__ uint2 lds[kQ8Lds];
+    __shared__ __align__(16) uint2 lds[kQ8Lds];               // read 16 bytes at a time
     const int lane = threadIdx.x & (kWaveSize - 1), wave = threadIdx.x >> 6;
     const int c0 = (blockIdx.y * G + (lane & (G - 1))) * kQ8Cols;
     const int8_t* codes = a.codes + min(c0, (a.F - 1) & -kQ8Cols);

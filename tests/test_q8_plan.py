@@ -138,3 +138,21 @@ def test_long_lists_of_rows_are_written_and_read_in_order(ask):
             assert first == (0 if q[4] else done), (q, line)
             done += rows
         assert done == q[2], (q, line)
+
+
+def test_staged_entries_are_aligned_for_16_byte_reads(tmp_path):
+    """Staged entries are read from LDS 16 bytes at a time: the arrays that hold them say so, wherever the compiler lays them."""
+    import re
+    from paper_2104_10716_amd import build
+    src = tmp_path / "aligned.hip"
+    src.write_text('#include "es_q8_spmm.h"\nnamespace {\n'
+                   'template __global__ void es_q8_few_kernel<4, false>(const Q8Args);\n'
+                   'template __global__ void es_q8_spmm_kernel<4, 32, true, false>(const Q8Args);\n'
+                   'template __global__ void es_q8_spmm_kernel<1, 4, false, false>(const Q8Args);\n}\n')
+    out = str(tmp_path / "aligned.ll")
+    flags = [f for f in build.HIPCC_FLAGS if f not in ("-O3", "-shared", "-fPIC", "-Wall", "-Wextra")]
+    subprocess.run([os.environ.get("HIPCC", "/opt/rocm/bin/hipcc"), "-w", "-O1", "-Xclang", "-disable-llvm-passes"] + flags +
+                   ["--cuda-device-only", "-S", "-emit-llvm", str(src), "-o", out], check=True, capture_output=True)
+    arrays = re.findall(r"^@(\S*E3lds) = .*addrspace\(3\) global .*, align (\d+)", open(out).read(), re.M)
+    assert len(arrays) == 3, arrays
+    assert all(int(align) >= 16 for _, align in arrays), arrays
