@@ -584,6 +584,12 @@ def _types():
     return {torch.float32: ES_FP32, torch.float16: ES_FP16, torch.bfloat16: ES_BF16}
 
 
+def _fit(value, bits=32) -> int:
+    """The nearest integer of so many bits (ctypes would keep the low ones): a W beyond every row stays one, and a size or
+    a code that the library refuses is still refused."""
+    return max(-2 ** (bits - 1), min(2 ** (bits - 1) - 1, int(value)))
+
+
 def _here(stream, **tensors):
     """The tensors are on the current device and can be read; returns the stream's address."""
     import torch
@@ -618,7 +624,7 @@ def _table(codes, scale, F):
     if codes.dtype != torch.int8 or scale.dtype != torch.float32:
         raise ValueError("codes must be int8 and scale float32")
     N, width, ldq = _matrix(codes, "codes")
-    row = int(load_library().es_q8_row_bytes(int(F)))
+    row = int(load_library().es_q8_row_bytes(_fit(F)))
     if width < row or ldq % 16 or codes.data_ptr() % 16:
         raise ValueError(f"codes must hold es_q8_row_bytes({F}) = {row} columns, 16-byte aligned, with a row stride that "
                          f"is a multiple of 16")
@@ -644,7 +650,7 @@ def _type_code(t, name):
 
 
 def _norm(norm) -> int:
-    return NORMS[norm] if isinstance(norm, str) else int(norm)
+    return NORMS[norm] if isinstance(norm, str) else _fit(norm)
 
 
 def _checked(rc, where):
@@ -682,7 +688,7 @@ def _workspace(workspace, need, stream):
 def es_q8_row_bytes(F: int) -> int:
     """Bytes of a row of F codes (F rounded up to 16): a table is
     torch.empty((N, es_q8_row_bytes(F)), dtype=torch.int8) and a float32 scale per row."""
-    return int(load_library().es_q8_row_bytes(int(F)))
+    return int(load_library().es_q8_row_bytes(_fit(F)))
 
 
 def es_q8_write(X, codes, scale, rows=None, stream=None):
@@ -732,7 +738,8 @@ def _q8_graph(rowptr, colidx, codes, scale, F):
 
 
 def es_spmm_q8_workspace_bytes(N: int, nnz: int, F: int, W: int, mode, n_rows: int) -> int:
-    return int(load_library().es_spmm_q8_workspace_bytes(int(N), int(nnz), int(F), int(W), _mode(mode), int(n_rows)))
+    return int(load_library().es_spmm_q8_workspace_bytes(_fit(N, 64), _fit(nnz, 64), _fit(F), _fit(W), _fit(_mode(mode)),
+                                                          _fit(n_rows, 64)))
 
 
 def es_spmm_q8(rowptr, colidx, vals, codes, scale, Y, W: int, mode, seed: int = 0, norm="none", rows=None, workspace=None,
@@ -754,12 +761,12 @@ def es_spmm_q8(rowptr, colidx, vals, codes, scale, Y, W: int, mode, seed: int = 
     if vals is not None and (vals.dtype != torch.float32 or vals.numel() != colidx.numel() or not vals.is_contiguous()):
         raise ValueError("vals must be contiguous float32, one per entry of colidx")
     lib = load_library()
-    need = int(lib.es_spmm_q8_workspace_bytes(N, colidx.numel(), F, int(W), _mode(mode), n)) if workspace is None else 0
+    need = es_spmm_q8_workspace_bytes(N, colidx.numel(), F, W, mode, n) if workspace is None else 0
     workspace, ws_bytes = _workspace(workspace, need, stream)
     _checked(lib.es_spmm_q8(
         rowptr.data_ptr() or None, colidx.data_ptr() or None, None if vals is None else vals.data_ptr() or None,
-        codes.data_ptr() or None, ldq, scale.data_ptr() or None, Y.data_ptr() or None, N, colidx.numel(), F, ldy, int(W),
-        _mode(mode), int(seed) & 0xFFFFFFFFFFFFFFFF, _norm(norm), _ids(rows, n), n,
+        codes.data_ptr() or None, ldq, scale.data_ptr() or None, Y.data_ptr() or None, N, colidx.numel(), F, ldy, _fit(W),
+        _fit(_mode(mode)), int(seed) & 0xFFFFFFFFFFFFFFFF, _norm(norm), _ids(rows, n), n,
         workspace.data_ptr() if ws_bytes else None, ws_bytes, st), "es_spmm_q8")
     return Y
 
@@ -781,13 +788,13 @@ def es_spmm_q8_backward_vals(rowptr, colidx, dY, codes, scale, dvals, W: int, mo
         raise ValueError("dvals must be contiguous float32, one per entry of colidx")
     _checked(load_library().es_spmm_q8_backward_vals(
         rowptr.data_ptr() or None, colidx.data_ptr() or None, dY.data_ptr() or None, ldy, codes.data_ptr() or None, ldq,
-        scale.data_ptr() or None, dvals.data_ptr() or None, N, colidx.numel(), F, int(W), _mode(mode),
+        scale.data_ptr() or None, dvals.data_ptr() or None, N, colidx.numel(), F, _fit(W), _fit(_mode(mode)),
         int(seed) & 0xFFFFFFFFFFFFFFFF, _norm(norm), st), "es_spmm_q8_backward_vals")
     return dvals
 
 
 def es_q8_weight_grad_workspace_bytes(N: int, F: int, H: int) -> int:
-    return int(load_library().es_q8_weight_grad_workspace_bytes(int(N), int(F), int(H)))
+    return int(load_library().es_q8_weight_grad_workspace_bytes(_fit(N, 64), _fit(F), _fit(H)))
 
 
 def es_q8_weight_grad(codes, scale, G, dW, workspace=None, stream=None):
@@ -806,9 +813,9 @@ def es_q8_weight_grad(codes, scale, G, dW, workspace=None, stream=None):
     if n != N:
         raise ValueError("G needs one row per row of codes")
     lib = load_library()
-    need = int(lib.es_q8_weight_grad_workspace_bytes(N, F, H)) if workspace is None else 0
+    need = es_q8_weight_grad_workspace_bytes(N, F, H) if workspace is None else 0
     workspace, ws_bytes = _workspace(workspace, need, stream)
     _checked(lib.es_q8_weight_grad(codes.data_ptr() or None, ldq, scale.data_ptr() or None, G.data_ptr() or None, ldg,
-                                   dW.data_ptr() or None, ldw, N, F, H, workspace.data_ptr() if ws_bytes else None, ws_bytes,
+                                   dW.data_ptr() or None, ldw, N, _fit(F), H, workspace.data_ptr() if ws_bytes else None, ws_bytes,
                                    st), "es_q8_weight_grad")
     return dW

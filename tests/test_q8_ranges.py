@@ -26,3 +26,43 @@ def test_more_rows_than_one_launch_takes(kind):
     assert torch.equal(es.es_q8_read(codes, scale, Y[:, :F], rows=ids), X.flip(0))
     es.es_q8_write(X, codes, scale, rows=ids)
     assert torch.equal(es.es_q8_read(codes, scale, Y[:, :F]), X.flip(0))
+
+
+def test_sizes_beyond_the_abi_are_not_cut_to_their_low_bits():
+    assert [es.es_q8_row_bytes(F) for F in (2 ** 32 + 16, 2 ** 64 + 16, -2 ** 32 + 16)] == [0, 0, 0]
+    ask = es.es_spmm_q8_workspace_bytes
+    assert ask(170_000, 2_400_000, 100, 0, "full", 170_000) > 0
+    for bad in ((2 ** 64 + 170_000, 2_400_000, 100, 0, "full", 170_000), (170_000, 2 ** 64 + 2_400_000, 100, 0, "full", 170_000),
+                (170_000, 2_400_000, 2 ** 32 + 100, 0, "full", 170_000), (170_000, 2_400_000, 100, 5000, 2 ** 32, 170_000),
+                (170_000, 2_400_000, 100, 0, "full", 2 ** 64 + 170_000), (170_000, 2_400_000, 100, -2 ** 32 + 5000, "bucket", 170_000)):
+        assert ask(*bad) == 0, bad
+    # a sample that is wider than any row can be is every row
+    assert ask(170_000, 2_400_000, 100, 2 ** 32 + 4, "bucket", 170_000) == ask(170_000, 2_400_000, 100, 2 ** 31 - 1, "bucket", 170_000) > 0
+    ask = es.es_q8_weight_grad_workspace_bytes
+    assert ask(1_000_000, 128, 128) > 0
+    assert ask(2 ** 64 + 1_000_000, 128, 128) == ask(1_000_000, 2 ** 32 + 128, 128) == ask(1_000_000, 128, 2 ** 32 + 128) == 0
+
+
+@pytest.mark.gpu
+def test_arguments_beyond_the_abi_are_not_cut_to_their_low_bits():
+    import torch
+    d = "cuda:0"
+    rowptr = torch.tensor([0, 3, 9, 9], dtype=torch.int32, device=d)
+    colidx = torch.tensor([0, 1, 2, 0, 1, 2, 2, 1, 0], dtype=torch.int32, device=d)
+    codes = torch.arange(-24, 24, dtype=torch.int8, device=d).reshape(3, 16)
+    scale = torch.tensor([1.0, 0.5, 2.0], device=d)
+    dY = torch.arange(48, dtype=torch.float32, device=d).reshape(3, 16)
+    new = lambda: torch.full((3, 16), 5.0, device=d)  # noqa: E731
+    want = es.es_spmm_q8(rowptr, colidx, None, codes, scale, new(), 0, "full")
+    da = es.es_spmm_q8_backward_vals(rowptr, colidx, dY, codes, scale, torch.empty(9, device=d), 0, "full")
+    for mode in ("bucket", "fastrand"):
+        for W in (2 ** 31, 2 ** 32 + 1, 2 ** 64 + 2):
+            assert torch.equal(es.es_spmm_q8(rowptr, colidx, None, codes, scale, new(), W, mode), want)
+            assert torch.equal(es.es_spmm_q8_backward_vals(rowptr, colidx, dY, codes, scale, torch.full((9,), 5.0, device=d), W, mode), da)
+    for W, mode, norm in ((4, 2 ** 32 + 1, "none"), (4, "bucket", 2 ** 32), (-2 ** 32 + 4, "bucket", "none")):
+        Y = new()
+        with pytest.raises(es.EsSpmmError):
+            es.es_spmm_q8(rowptr, colidx, None, codes, scale, Y, W, mode, 0, norm)
+        with pytest.raises(es.EsSpmmError):
+            es.es_spmm_q8_backward_vals(rowptr, colidx, dY, codes, scale, torch.empty(9, device=d), W, mode, 0, norm)
+        assert bool((Y == 5.0).all())
