@@ -494,9 +494,11 @@ int es_q8_read(const int8_t* codes, int32_t ldq, const float* scale, int64_t N, 
  *           irrelevant, on return unspecified; calls that share it must be ordered
  *           (same stream).  With a smaller one, or none, such a row is one workgroup's.
  * Accumulation is fp32 in an order that the sizes and the workspace fix: the same
- * call gives the same bits.  A row of the table that no kept entry names has no
- * influence, whatever it holds.  ES_ERR_UNSUPPORTED for F above 16 776 960, and where the
- * rows are more than a launch holds (never up to 700 million).
+ * call gives the same bits.  vals[p] * scale is rounded to fp32 before the code comes to
+ * it: where it overflows, columns whose code is 0 come out as NaN.  A row of the table
+ * that no kept entry names has no influence, whatever it holds.  ES_ERR_UNSUPPORTED for F
+ * above 16 776 960, and where the rows are more than a launch holds (never up to 700
+ * million).
  */
 size_t es_spmm_q8_workspace_bytes(int64_t N, int64_t nnz, int32_t F, int32_t W, int32_t mode,
                                   int64_t n_rows);
@@ -530,8 +532,9 @@ int es_spmm_q8_backward_vals(const int32_t* rowptr, const int32_t* colidx,
  * es_q8_weight_grad -- dW = X^T * G with X held as 8-bit rows: the weight gradient of a
  * dense layer Z = X * W (Equation 1's H * W) from the checkpoint of its input.
  *   G       N rows of H fp32, row stride ldg >= H: the gradient with respect to Z; meant
- *           to hold finite values: an element of dW whose exact value is +-Inf may come
- *           out as NaN.  ldg and ldq below 2^27.
+ *           to hold finite values whose products with the scales are finite: other
+ *           elements of dW may come out as NaN.  What scale * G has below 2^-133 is lost.
+ *           ldg below 2^26 and ldq below 2^27 (ES_ERR_UNSUPPORTED).
  *   dW      F rows of H fp32, row stride ldw >= H, overwritten (zeros for N == 0)
  *   workspace  es_q8_weight_grad_workspace_bytes(N, F, H) bytes (0: none is of use),
  *           16-byte aligned; contents on entry are irrelevant, on return unspecified;

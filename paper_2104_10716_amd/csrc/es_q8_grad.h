@@ -3,17 +3,19 @@
 //   dW[i, j] = sum over r of code[r, i] * (scale[r] * G[r, j])
 //
 // On the matrix cores in bf16, exactly: a code has 8 significant bits and is a bf16 number; g = scale * G, rounded once to
-// fp32, is the sum of three bf16 numbers, its leading, middle and last 8 bits (as long as the last are no subnormals, from
-// |g| of 2^-102 on); every product of the two is exact in fp32.  What is rounded is g and the sums, in fp32.
+// fp32, is the sum of three bf16 numbers, its leading, middle and last 8 bits (exactly from |g| of 2^-110 on; bf16 ends at
+// 2^-133, and bits of g below that are lost); every product of the two is exact in fp32.  What is rounded is g and the sums, in fp32.
 //
 // A matrix instruction wants 8 rows r of one column i (or j) in a lane's registers, and in memory a row's columns lie
 // side by side.  No data has to be turned for that: a lane loads the same 4 columns of codes (2 of G) of 8 rows, and
 // registers number c of those loads are what the lane owes the c-th of 4 (2) tiles; which 32 columns
 // a tile then has, every fourth (second), is of no consequence until the result is stored.  A narrow dW takes fewer tiles.
 //
-// 233 k rows, 602 x 256: 250 us and 9 us of join, 0.86 PFLOP/s of the three products, bound by the matrix cores at the clock that
-// they hold under load (neither without its conversions nor with operands shared through LDS was the kernel faster); 2.45 M rows,
-// 128 x 128: 280 us and 4 us, bound by HBM (5.2 TB/s).
+// 233 k rows, 602 x 256: 250 us and 9 us of join, 0.86 PFLOP/s of the three products.  Of its 548 k clocks (2.14 GHz) the matrix cores
+// are busy for 40 %, and the vector ALUs, which convert and split the operands, for about as many; 10 % of the waves' time is waiting for
+// memory.  That is most of the time if the two waves of a SIMD overlap the one with the other as little as it looks; the matrix cores' rate
+// alone does not bound it (a library's bf16 product of 8192^3: 69 % at 1.69 GHz).  2.45 M rows, 128 x 128: 280 us and 4 us, bound by HBM (5.2
+// TB/s).
 #ifndef ES_SPMM_Q8_GRAD_H
 #define ES_SPMM_Q8_GRAD_H
 

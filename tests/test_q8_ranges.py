@@ -66,3 +66,26 @@ def test_arguments_beyond_the_abi_are_not_cut_to_their_low_bits():
         with pytest.raises(es.EsSpmmError):
             es.es_spmm_q8_backward_vals(rowptr, colidx, dY, codes, scale, torch.empty(9, device=d), W, mode, 0, norm)
         assert bool((Y == 5.0).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("exponent", [-95, -105, -110, -111, -118, -126, -130, -140])
+def test_weight_gradient_of_very_small_numbers(exponent):
+    """scale * G goes to the matrix cores as three bf16 numbers, whose last place is 2^-133: what is below it is lost, at
+    most |code| 2^-133 per product, beside the roundings of any other sum (three per row).  From 2^-110 on nothing is below it."""
+    import numpy as np
+    import torch
+    N, F, H = 200, 40, 70
+    rng = np.random.default_rng(-exponent)
+    q = rng.integers(-127, 128, (N, F)).astype(np.int8)
+    s = np.exp2(rng.integers(-3, 4, N)).astype(np.float32)
+    g = (rng.uniform(1, 2, (N, H)) * np.exp2(exponent) / s[:, None]).astype(np.float32) * rng.choice([-1, 1], (N, H)).astype(np.float32)
+    codes = torch.zeros((N, 48), dtype=torch.int8, device="cuda:0")
+    codes[:, :F] = torch.from_numpy(q).cuda()
+    dW = es.es_q8_weight_grad(codes, torch.from_numpy(s).cuda(), torch.from_numpy(g).cuda(), torch.empty((F, H), device="cuda:0"))
+    x, y = q.astype(np.float64), g.astype(np.float64) * s.astype(np.float64)[:, None]
+    tol = np.abs(x).T @ np.abs(y) * (3 * N + 8) * 2.0 ** -24 + (N + 1) * 2.0 ** -150
+    if exponent < -110:
+        tol += np.abs(x).sum(0)[:, None] * 2.0 ** -133
+    err = np.abs(dW.cpu().numpy().astype(np.float64) - x.T @ y)
+    assert (err <= 1.01 * tol).all(), (err / tol).max()
