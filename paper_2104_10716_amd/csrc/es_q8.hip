@@ -163,16 +163,17 @@ int check_product(int64_t N, int64_t nnz, int32_t F, int32_t ldq, int32_t ld, in
 
 // Lanes to a row.  As few as cover its columns leave little to sum across lanes and the fewest lanes idle; half a wave
 // is done with a row sooner, which counts where rows are few, or long and of very different lengths (uniform ids, us with G or 4 lanes /
-// 32 / 64; m: mean kept):
-//  * 2700 rows, exact, F = 16, m = 5: 15.6 / 7.5 / 7.7, F = 64, m = 30: 18.9 / 10.4 / 9.3, m = 100: 45 / 12.1 / 10.5; 8000 rows: 15.6 /
-//    8.5 / 9.5, 19.5 / 13.9 / 12.5, 52 / 20 / 20; 20 k rows: 20 / 15.5 / 18, 33 / 27 / 27, 97 / 54 / 54
-//  * 60 k rows, m = 5: 23 / 25 / 37, F = 64, m = 30: 61 / 51 / 56, F = 128, FastRand, m = 100: 70 / 54 / 55
-//  * 233 k rows, F = 64, m = 30: 168 / 162 / 190, Bucket m = 24: 60 / 74 / 119, exact m = 490: 2401 / 1887 / 1934, F = 128: 2487 / 2184 /
-//    2223, FastRand m = 200: 545 / 485 / 453, Bucket m = 32: 115 / 133 / 134, F = 256, m = 490: 4360 / 4402 / 4496
-//  * 700 k rows, F = 64, m = 30: 589 / 628 / 693, F = 19, Bucket m = 60: 645 / 614 / 628, F = 128, m = 60: 1177 / 1236 / 1259, FastRand
-//    m = 150: 1658 / 1544 / 1456; 2.45 M, F = 128, FastRand m = 50: 1359 / 1519 / 1505
-// The edge gradient: 2700 rows, F = 64, m = 30: 20 / 9.7 / 8.0; 20 k: 28 / 22 / 21; 233 k, F = 64, m = 100: 542 / 401 / 425, F = 128, m = 5:
-// 67 / 118 / 191.
+// 32 / 64; m: mean length of the whole rows):
+//  * exact, 2700 rows, F = 16, m = 5: 15.2 / 8.2 / 8.9, F = 64, m = 30: 18.8 / 10.1 / 9.3, m = 100: 45 / 12.4 / 10.8; 8000 rows: 15.6 /
+//    8.3 / 9.6, 19.2 / 13.8 / 12.6, 51 / 20 / 20; 20 k rows: 17.8 / 14.1 / 17.5, 29 / 23 / 22, 82 / 41 / 40
+//  * 60 k rows, F = 16, m = 5: 22 / 25 / 37, F = 64, m = 30: 56 / 48 / 55, F = 128, FastRand of 100, m = 100: 70 / 53 / 59
+//  * 233 k rows, F = 64, m = 30: 162 / 148 / 172, Bucket 24: 60 / 64 / 112, exact, m = 490: 2402 / 1843 / 1827, F = 128: 2483 / 2137 /
+//    2098, FastRand of 200, m = 200: 546 / 452 / 421, Bucket 32, m = 490: 111 / 117 / 124, F = 256, exact: 4365 / 4326 / 4415
+//  * 700 k rows, F = 64, m = 30: 581 / 583 / 596, F = 19, Bucket 60, m = 150: 824 / 756 / 759, F = 128, m = 60: 1172 / 1187 / 1171, FastRand
+//    of 200, m = 150: 1638 / 1528 / 1414; 2.45 M, F = 128, FastRand of 64, m = 49: 2151 / 2247 / 2131
+// The edge gradient: 2700 rows, F = 64, m = 30: 19.8 / 9.4 / 7.9; 20 k: 28 / 22 / 22; 233 k, F = 64, m = 100: 545 / 401 / 415, F = 128, m = 5:
+// 66 / 99 / 144.
+// The rule goes by the mean kept; of these it loses 8 % (233 k, F = 64, m = 30), 7 % (FastRand of 200 on 233 k rows) and 14 % (on 700 k).
 int pick_team(int G, int64_t n_rows, double mean)
 {
     const int least = G < 4 ? 4 : G;
@@ -185,11 +186,11 @@ int pick_team(int G, int64_t n_rows, double mean)
 
 // The same for the edge gradient of FastRand, whose kept entries wait in LDS: 256 of a row with 16 lanes, 512 with 32, 1024 with 64.
 // The wider the sample, the more its rows differ in length.  16 / 32 / 64 lanes, us (m: mean of the whole row):
-//  * 2700 rows, m = 14, F = 100, W = 100: 13.5 / 9.4 / 8.5; 8000 rows, m = 5, F = 16, W = 50: 7.3 / 7.0 / 8.2, m = 30, F = 128, W = 200: 26 / 19 / 15
-//  * 60 k rows, m = 5, F = 128, W = 50: 33 / 35 / 46, m = 14, F = 100, W = 100: 50 / 48 / 60, m = 100, F = 128, W = 250: 130 / 97 / 90; F = 300,
-//    m = 30, W = 16: - / 61 / 71, F = 400, W = 500: - / 248 / 203
-//  * 233 k rows, m = 5, F = 128, W = 50: 94 / 114 / 160, m = 30, W = 200: 167 / 160 / 198, m = 100, W = 250: 315 / 304 / 315; F = 300, W = 16: - / 228 / 280,
-//    F = 400, W = 500: - / 593 / 569; 700 k, m = 14, F = 100, W = 100: 416 / 522 / 793, m = 30, F = 128, W = 200: 461 / 485 / 625
+//  * 2700 rows, m = 14, F = 100, W = 100: 13.1 / 9.0 / 8.0; 8000 rows, m = 5, F = 16, W = 50: 7.2 / 7.0 / 8.2, m = 30, F = 128, W = 200: 25 / 19 / 15
+//  * 60 k rows, m = 5, F = 128, W = 50: 33 / 35 / 53, m = 14, F = 100, W = 100: 50 / 47 / 68, m = 100, F = 128, W = 250: 128 / 95 / 97; F = 300,
+//    m = 30, W = 16: - / 60 / 80, F = 400, W = 500: - / 245 / 191
+//  * 233 k rows, m = 5, F = 128, W = 50: 93 / 111 / 155, m = 30, W = 200: 167 / 157 / 194, m = 100, W = 250: 312 / 304 / 293; F = 300, W = 16: - / 227 / 278,
+//    F = 400, W = 500: - / 588 / 537; 700 k, m = 14, F = 100, W = 100: 412 / 519 / 658, m = 30, F = 128, W = 200: 460 / 481 / 597
 int pick_random_team(int G, int64_t n_rows, int32_t W)
 {
     const bool many = n_rows > 98'304;
